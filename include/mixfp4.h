@@ -472,13 +472,116 @@ int mixfp4_decode_step(const uint16_t *a, int64_t m, int64_t k, const uint8_t *w
                        uint8_t *a_codes, uint8_t *a_scales, float *a_tensor_scale, float *c,
                        uint32_t *sync, void *stream);
 
+/*
+ * Dropout whose mask is drawn again wherever it is needed and never stored.
+ *
+ * Element (i, j) of a [rows, k] matrix has a 16-bit draw: half j % 2 (low
+ * first) of word (j % 8) / 2 of Philox4x32-10 under the key `seed` and the
+ * counter (i ceil(k / 8) + j / 8, offset), both counters 64-bit, low word
+ * first.  It is kept when the draw is at least T = p 65536 rounded to nearest
+ * (0 <= p <= 1, anything else is MIXFP4_ERR_SHAPE), and kept elements are
+ * multiplied by z = 65536 / (65536 - T).  A dropped element counts as zero
+ * whatever it holds.  The draws depend on (seed, offset, i, j, k) alone.
+ *
+ * mixfp4_dropout - out = residual + z keep x, computed in fp32 and rounded
+ * once.  The backward pass is the same call on the gradient, without the
+ * residual.
+ *   x, residual, out  matrices [rows, k] of row pitch ldx, ldr, ldo >= k
+ *                     elements; MIXFP4_TYPE_F32 or MIXFP4_TYPE_BF16 each,
+ *                     aligned to their element (rows that begin on 16 bytes
+ *                     are read and written fastest).  residual NULL: none.
+ *                     out may be x or residual itself if type and pitch are
+ *                     the same.  Infinities and NaN are taken.
+ *   rows, k           >= 0, k <= 2^32; nothing is written if one is 0.
+ */
+#define MIXFP4_TYPE_F32 0
+#define MIXFP4_TYPE_BF16 1
+int mixfp4_dropout(const void *x, int32_t x_type, int64_t ldx,
+                   const void *residual, int32_t residual_type, int64_t ldr,
+                   void *out, int32_t out_type, int64_t ldo, int64_t rows,
+                   int64_t k, double p, uint64_t seed, uint64_t offset,
+                   void *stream);
+
+/*
+ * Low-rank adapters beside a shared projection, many of them in one call.
+ *
+ * Row i of X [m, k] has the adapter l = index[i]; rows whose index is outside
+ * [0, adapters) have none.  With A_l [rank, k], B_l [n, rank], the scaling s_l,
+ * dropout's keep mask on X and z as above:
+ *   t_i  = z (keep_i x_i) A_l^T            out_i = c_i + s_l t_i B_l^T
+ *   u_i  = s_l dy_i B_l                    dx_i  = dx_in_i + z keep_i (u_i A_l)
+ *   dA_l = z sum_i u_i^T (keep_i x_i)      dB_l  = s_l sum_i dy_i^T t_i
+ * Rows without an adapter get out = c, t = 0 and dx = dx_in; adapters without
+ * rows get gradients of zero.  Sums are fp32; t and u enter the products
+ * behind them as bf16 terms, two for out and dx (relative error 2^-17), three
+ * for dA and dB.  Results are deterministic.  Infinities and NaN are taken; they stay within what depends
+ * on them.
+ *
+ * mixfp4_adapter_plan - the rows grouped by adapter, for any number of calls
+ * on the same rows (every projection of a batch).
+ *   index       int32 [rows], 4-byte aligned.
+ *   rows        0 .. 2^28.   adapters  1 .. 4096.
+ *   plan        out: mixfp4_adapter_plan_bytes(rows, adapters) bytes, 16-byte
+ *               aligned; a smaller plan_bytes is MIXFP4_ERR_SHAPE.
+ *
+ * mixfp4_adapter - the forward pass.
+ *   x           bf16 [m, k], pitch ldx >= k, ldx % 8 == 0, 16-byte aligned.
+ *   a, b        bf16 [adapters, rank, k] and [adapters, n, rank], contiguous,
+ *               16-byte aligned; rank 8 .. 256, rank % 8 == 0; k 8 .. 2^22,
+ *               k % 8 == 0; n 1 .. 2^22.
+ *   scaling     fp32 [adapters], or NULL for 1.
+ *   ranks       int32 [adapters], or NULL: adapter l uses the first ranks[l]
+ *               (held to 0 .. rank) rows of A_l and columns of B_l; the others
+ *               are not looked at, and their t and gradients are zero.
+ *   plan        of mixfp4_adapter_plan for the same m and adapters.
+ *   c           fp32 [m, n], pitch ldc >= n (mixfp4_gemm's output), or NULL
+ *               for zero.
+ *   t           out: fp32 [m, rank] contiguous for the backward pass, or NULL.
+ *   out         [m, n], fp32 or bf16 (out_type), pitch ldo >= n; may be c
+ *               itself (fp32, ldo == ldc).
+ *   workspace   mixfp4_adapter_workspace_size's forward_bytes, 256-byte
+ *               aligned; calls that overlap in time need one each.
+ *
+ * mixfp4_adapter_backward - the backward pass for the gradient dY of out, with
+ * the forward pass's x, t, p, seed and offset.
+ *   dy          bf16 [m, n], pitch lddy >= n, lddy % 8 == 0, 16-byte aligned.
+ *   dx_in       fp32 [m, k] (the projection's own input gradient), pitch
+ *               lddx_in >= k, or NULL for zero.
+ *   dx          out: fp32 [m, k], pitch lddx >= k; may be dx_in itself.
+ *   da, db      out: fp32, the shapes of a and b, contiguous, 16-byte aligned.
+ *   workspace   backward_bytes.
+ * m == 0 writes no rows (and gradients of zero).
+ */
+int mixfp4_adapter_plan_bytes(int64_t rows, int64_t adapters, int64_t *bytes);
+int mixfp4_adapter_plan(const int32_t *index, int64_t rows, int64_t adapters,
+                        void *plan, int64_t plan_bytes, void *stream);
+int mixfp4_adapter_workspace_size(int64_t m, int64_t n, int64_t k, int64_t rank,
+                                  int64_t adapters, int64_t *forward_bytes,
+                                  int64_t *backward_bytes);
+int mixfp4_adapter(const uint16_t *x, int64_t ldx, const uint16_t *a,
+                   const uint16_t *b, const float *scaling, const int32_t *ranks,
+                   const void *plan, const float *c, int64_t ldc, int64_t m,
+                   int64_t n, int64_t k, int64_t rank, int64_t adapters,
+                   double p, uint64_t seed, uint64_t offset, float *t, void *out,
+                   int32_t out_type, int64_t ldo, void *workspace,
+                   int64_t workspace_bytes, void *stream);
+int mixfp4_adapter_backward(const uint16_t *dy, int64_t lddy, const uint16_t *x,
+                            int64_t ldx, const float *t, const uint16_t *a,
+                            const uint16_t *b, const float *scaling,
+                            const int32_t *ranks, const void *plan,
+                            const float *dx_in, int64_t lddx_in, int64_t m,
+                            int64_t n, int64_t k, int64_t rank, int64_t adapters,
+                            double p, uint64_t seed, uint64_t offset, float *dx,
+                            int64_t lddx, float *da, float *db, void *workspace,
+                            int64_t workspace_bytes, void *stream);
+
 /* HIP error string of the last MIXFP4_ERR_LAUNCH on the calling thread. */
 const char *mixfp4_last_launch_error(void);
 
 /* ABI version of this header (major * 100 + minor). */
 int mixfp4_abi_version(void);
 
-#define MIXFP4_ABI_VERSION 110
+#define MIXFP4_ABI_VERSION 111
 
 #ifdef __cplusplus
 }

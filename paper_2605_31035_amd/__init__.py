@@ -24,6 +24,11 @@ Functions (same names as the C ABI in include/mixfp4.h):
   mixfp4_decode_operand((codes, scales, s32)) -> Decoded (the operand decoded
       once to exact 16-bit values in the library's blocked layout)
   mixfp4_gemm_decoded(a: Decoded, w: Decoded) -> C = A W^T (fp32)
+  mixfp4_dropout(x, residual=None, p=.., seed=.., offset=..) -> residual + dropout(x)
+  mixfp4_adapter_plan(index, adapters) -> AdapterPlan (rows grouped by adapter)
+  mixfp4_adapter(x, a, b, plan, c=None, ...) -> c + scaling dropout(x) A^T B^T,
+      each row with its own low-rank adapter
+  mixfp4_adapter_backward(dy, x, t, a, b, plan, dx=None, ...) -> (dx, da, db)
 """
 from __future__ import annotations
 
@@ -40,7 +45,8 @@ __all__ = ["mixfp4_decode_step", "decode_step_applies", "gemm_two_pass_preferred
            "FORCE_E2M1", "FORCE_E1M2", "STOCHASTIC", "TRANSPOSE", "mixfp4_quantize_2d",
            "mixfp4_gemm_workspace_size", "mixfp4_decode_operand", "mixfp4_gemm_decoded",
            "Decoded", "mixfp4_quantize_variant", "mixfp4_dequantize_variant", "Variant",
-           "CANDIDATES", "mixfp4_quantize_decode"]
+           "CANDIDATES", "mixfp4_quantize_decode", "mixfp4_dropout", "AdapterPlan",
+           "mixfp4_adapter_plan", "mixfp4_adapter", "mixfp4_adapter_backward"]
 
 SCALE_COMPUTE = 0
 SCALE_GIVEN = 1
@@ -601,3 +607,256 @@ def mixfp4_gemm_decoded(a: Decoded, w: Decoded, out: torch.Tensor | None = None)
     _check(lib.mixfp4_gemm_decoded(_ptr(a.buf), _ptr(a.s32), _ptr(w.buf), _ptr(w.s32), m, n, a.k,
                                    _ptr(out), _stream(a.buf.device)))
     return out
+
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _pitch(t, name: str, dtypes, shape, multiple: int = 1) -> int:
+    """Check a caller's matrix and return its row pitch in elements."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D tensor")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must be {' or '.join(map(str, dtypes))}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    rows, cols = shape
+    if cols > 1 and rows > 0 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit stride along its rows")
+    if rows <= 1:
+        return -(-cols // 8) * 8
+    if t.stride(0) < cols or t.stride(0) % multiple:
+        raise ValueError(f"{name}'s rows must not overlap and start at multiples of {multiple} "
+                         f"elements, got a pitch of {t.stride(0)}")
+    return t.stride(0)
+
+
+def _apart(out, *named, same=None):
+    """An output may be `same` itself (its address and pitch) and must not
+    share memory with the inputs otherwise."""
+    if out is None or out.numel() == 0:
+        return
+
+    def span(t):
+        # from the first element to behind the last one
+        return t.data_ptr(), t.data_ptr() + t.element_size() * (
+            1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
+
+    lo, hi = span(out)
+    for name, t in named:
+        if t is None or t.numel() == 0 or t.device != out.device:
+            continue
+        if t is same and t.data_ptr() == lo and t.dtype == out.dtype and t.shape == out.shape \
+                and (t.shape[0] == 1 or t.stride() == out.stride()):
+            continue
+        a, b = span(t)
+        if a < hi and lo < b:
+            raise ValueError(f"the output shares memory with {name}")
+
+
+def _launch(dev, call, *args):
+    """The library call on the device's current stream, with the device made
+    current meanwhile."""
+    if dev.index is None or dev.index == torch.cuda.current_device():
+        _check(call(*args, _stream(dev)))
+    else:
+        with torch.cuda.device(dev):
+            _check(call(*args, _stream(dev)))
+
+
+def _probability(p) -> float:
+    p = float(p)
+    if not 0.0 <= p <= 1.0:
+        raise ValueError(f"p must be in 0 .. 1, got {p}")
+    return p
+
+
+def _u64(v: int) -> int:
+    return int(v) & 0xFFFFFFFFFFFFFFFF
+
+
+def mixfp4_dropout(x: torch.Tensor, residual: torch.Tensor | None = None, p: float = 0.5,
+                   seed: int = 0, offset: int = 0, out_dtype: torch.dtype | None = None,
+                   out: torch.Tensor | None = None) -> torch.Tensor:
+    """residual + dropout(x) for a [rows, k] CUDA tensor, without a stored
+    mask (mixfp4_dropout): an element is kept by its own 16-bit Philox draw of
+    (``seed``, ``offset``) and multiplied by 1 / (1 - p), p rounded to a
+    65536th.  x, residual and the result are float32 or bfloat16 each, with
+    any row pitch; ``out_dtype`` (default: x's) the result's type.  ``out`` may
+    be x or residual itself.  The gradient of x is
+    ``mixfp4_dropout(dy, p=p, seed=seed, offset=offset)``."""
+    p = _probability(p)
+    if out is not None:
+        if out_dtype is not None and isinstance(out, torch.Tensor) and out.dtype != out_dtype:
+            raise ValueError(f"out must be {out_dtype}, got {out.dtype}")
+    elif out_dtype is not None and out_dtype not in _TYPES:
+        raise ValueError("out_dtype must be torch.float32 or torch.bfloat16")
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("x must be a 2-D tensor")
+    shape, types = tuple(x.shape), tuple(_TYPES)
+    ldx = _pitch(x, "x", types, shape)
+    ldr = _pitch(residual, "residual", types, shape) if residual is not None else 0
+    if out is None:
+        if not x.is_cuda:
+            raise ValueError("x must be a CUDA tensor")
+        out = torch.empty(shape, dtype=out_dtype or x.dtype, device=x.device)
+    ldo = _pitch(out, "out", types, shape)
+    _same_device(x.device, ("x", x), ("residual", residual), ("out", out))
+    _apart(out, ("x", x), same=x)
+    _apart(out, ("residual", residual), same=residual)
+    _launch(x.device, lib.mixfp4_dropout, _ptr(x), _TYPES[x.dtype], ldx, _ptr(residual),
+            _TYPES[residual.dtype] if residual is not None else 0, ldr, _ptr(out),
+            _TYPES[out.dtype], ldo, *shape, p, _u64(seed), _u64(offset))
+    return out
+
+
+class AdapterPlan(NamedTuple):
+    """Rows grouped by adapter (mixfp4_adapter_plan): ``buf`` (uint8 CUDA
+    tensor in the library's layout), the number of rows and of adapters."""
+    buf: torch.Tensor
+    rows: int
+    adapters: int
+
+
+def mixfp4_adapter_plan(index: torch.Tensor, adapters: int) -> AdapterPlan:
+    """Group the rows of a batch by their adapter: ``index`` int32 [m], row
+    i's adapter, or anything outside [0, adapters) for none.  The plan serves
+    any number of calls on these rows (every adapted projection of the
+    batch)."""
+    if not isinstance(index, torch.Tensor) or index.dim() != 1:
+        raise ValueError("index must be a 1-D int32 tensor")
+    m, adapters = index.shape[0], int(adapters)
+    _require(index, "index", torch.int32)
+    need = ctypes.c_int64(0)
+    _check(lib.mixfp4_adapter_plan_bytes(m, adapters, ctypes.byref(need)))
+    _same_device(index.device, ("index", index))
+    buf = torch.empty(need.value, dtype=torch.uint8, device=index.device)
+    _launch(index.device, lib.mixfp4_adapter_plan, _ptr(index), m, adapters, _ptr(buf), need.value)
+    return AdapterPlan(buf, m, adapters)
+
+
+def _adapter_weights(a, b, plan, scaling, ranks, m: int, k: int):
+    """Check A, B, the plan and the per-adapter vectors; (n, rank, adapters)."""
+    if not isinstance(a, torch.Tensor) or a.dim() != 3 or not isinstance(b, torch.Tensor) \
+            or b.dim() != 3:
+        raise ValueError("a must be [adapters, rank, k] and b [adapters, n, rank]")
+    adapters, rank = a.shape[:2]
+    n = b.shape[1]
+    _require(a, "a", torch.bfloat16, (adapters, rank, k))
+    _require(b, "b", torch.bfloat16, (adapters, n, rank))
+    if rank % 8 or not 8 <= rank <= 256:
+        raise ValueError(f"the rank must be a multiple of 8 in 8 .. 256, got {rank}")
+    if k % 8 or k < 8 or n < 1:
+        raise ValueError(f"k must be a multiple of 8 and n at least 1, got k={k}, n={n}")
+    if not isinstance(plan, AdapterPlan):
+        raise ValueError("plan must be an AdapterPlan (mixfp4_adapter_plan)")
+    if plan.rows != m or plan.adapters != adapters:
+        raise ValueError(f"the plan is for {plan.rows} rows and {plan.adapters} adapters, "
+                         f"not {m} and {adapters}")
+    need = ctypes.c_int64(0)
+    _check(lib.mixfp4_adapter_plan_bytes(m, adapters, ctypes.byref(need)))
+    _require(plan.buf, "plan", torch.uint8, numel=need.value)
+    if scaling is not None:
+        _require(scaling, "scaling", torch.float32, (adapters,))
+    if ranks is not None:
+        _require(ranks, "ranks", torch.int32, (adapters,))
+    return n, rank, adapters
+
+
+def _adapter_workspace(m, n, k, rank, adapters, backward: bool) -> int:
+    b = ctypes.c_int64(0)
+    fwd, bwd = (None, ctypes.byref(b)) if backward else (ctypes.byref(b), None)
+    _check(lib.mixfp4_adapter_workspace_size(m, n, k, rank, adapters, fwd, bwd))
+    return max(1, b.value)
+
+
+def mixfp4_adapter(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, plan: AdapterPlan,
+                   c: torch.Tensor | None = None, scaling: torch.Tensor | None = None,
+                   ranks: torch.Tensor | None = None, p: float = 0.0, seed: int = 0,
+                   offset: int = 0, out_dtype: torch.dtype | None = None, keep_t: bool = False,
+                   out: torch.Tensor | None = None):
+    """out = c + scaling_l dropout(x) A_l^T B_l^T, row by row with the row's own
+    adapter l (mixfp4_adapter): low-rank adapters of many requests beside the
+    shared projection whose output is c.
+
+    ``x`` bf16 [m, k] (the projection's input), ``a`` bf16 [adapters, rank, k],
+    ``b`` bf16 [adapters, n, rank], ``plan`` mixfp4_adapter_plan of the rows,
+    ``c`` fp32 [m, n] (mixfp4_gemm's result) or None for zero, ``scaling`` fp32
+    [adapters] or None for 1, ``ranks`` int32 [adapters] for adapters of smaller
+    ranks (what a and b hold behind them is not looked at), ``p``, ``seed`` and
+    ``offset`` as for mixfp4_dropout.  ``out_dtype`` float32 (default) or
+    bfloat16; ``out`` may be c itself.  Rows without an adapter get c.
+    Returns out [m, n], with ``keep_t`` (out, t): t fp32 [m, rank], what the
+    backward pass needs of this one."""
+    p = _probability(p)
+    if out_dtype is not None and out_dtype not in _TYPES:
+        raise ValueError("out_dtype must be torch.float32 or torch.bfloat16")
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("x must be a 2-D tensor")
+    m, k = x.shape
+    ldx = _pitch(x, "x", (torch.bfloat16,), (m, k), 8)
+    n, rank, adapters = _adapter_weights(a, b, plan, scaling, ranks, m, k)
+    ldc = _pitch(c, "c", (torch.float32,), (m, n)) if c is not None else 0
+    if out is None:
+        if not x.is_cuda:
+            raise ValueError("x must be a CUDA tensor")
+        out = torch.empty((m, n), dtype=out_dtype or torch.float32, device=x.device)
+    elif out_dtype is not None and isinstance(out, torch.Tensor) and out.dtype != out_dtype:
+        raise ValueError(f"out must be {out_dtype}, got {out.dtype}")
+    ldo = _pitch(out, "out", tuple(_TYPES), (m, n))
+    _same_device(x.device, ("x", x), ("a", a), ("b", b), ("plan", plan.buf), ("c", c),
+                 ("scaling", scaling), ("ranks", ranks), ("out", out))
+    _apart(out, ("x", x), ("a", a), ("b", b), ("c", c), ("plan", plan.buf), ("scaling", scaling),
+           ("ranks", ranks), same=c)
+    dev = x.device
+    t = torch.empty((m, rank), dtype=torch.float32, device=dev) if keep_t else None
+    need = _adapter_workspace(m, n, k, rank, adapters, False)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    _launch(dev, lib.mixfp4_adapter, _ptr(x), ldx, _ptr(a), _ptr(b), _ptr(scaling), _ptr(ranks),
+            _ptr(plan.buf), _ptr(c), ldc, m, n, k, rank, adapters, p, _u64(seed), _u64(offset),
+            _ptr(t), _ptr(out), _TYPES[out.dtype], ldo, _ptr(ws), need)
+    return (out, t) if keep_t else out
+
+
+def mixfp4_adapter_backward(dy: torch.Tensor, x: torch.Tensor, t: torch.Tensor, a: torch.Tensor,
+                            b: torch.Tensor, plan: AdapterPlan, dx: torch.Tensor | None = None,
+                            scaling: torch.Tensor | None = None,
+                            ranks: torch.Tensor | None = None, p: float = 0.0, seed: int = 0,
+                            offset: int = 0, out: torch.Tensor | None = None):
+    """Gradients of mixfp4_adapter for dY (mixfp4_adapter_backward): (dx_in + the
+    adapters' gradient of x fp32 [m, k], dA fp32 [adapters, rank, k], dB fp32
+    [adapters, n, rank]).
+
+    ``dy`` bf16 [m, n] with rows that start at multiples of 8 elements, ``x``,
+    ``plan``, ``scaling``, ``ranks``, ``p``, ``seed`` and ``offset`` of the forward
+    call and ``t`` what it kept; ``dx`` fp32 [m, k] the shared projection's own
+    input gradient (DGRAD's result) or None for zero; ``out`` where the new one
+    goes, which may be ``dx`` itself."""
+    p = _probability(p)
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("x must be a 2-D tensor")
+    m, k = x.shape
+    ldx = _pitch(x, "x", (torch.bfloat16,), (m, k), 8)
+    n, rank, adapters = _adapter_weights(a, b, plan, scaling, ranks, m, k)
+    lddy = _pitch(dy, "dy", (torch.bfloat16,), (m, n), 8)
+    _require(t, "t", torch.float32, (m, rank))
+    lddx_in = _pitch(dx, "dx", (torch.float32,), (m, k)) if dx is not None else 0
+    if out is None:
+        if not x.is_cuda:
+            raise ValueError("x must be a CUDA tensor")
+        out = torch.empty((m, k), dtype=torch.float32, device=x.device)
+    lddx = _pitch(out, "out", (torch.float32,), (m, k))
+    _same_device(x.device, ("dy", dy), ("x", x), ("t", t), ("a", a), ("b", b), ("plan", plan.buf),
+                 ("dx", dx), ("scaling", scaling), ("ranks", ranks), ("out", out))
+    _apart(out, ("dy", dy), ("x", x), ("t", t), ("a", a), ("b", b), ("dx", dx), ("plan", plan.buf),
+           ("scaling", scaling), ("ranks", ranks), same=dx)
+    dev = x.device
+    da = torch.empty(a.shape, dtype=torch.float32, device=dev)
+    db = torch.empty(b.shape, dtype=torch.float32, device=dev)
+    need = _adapter_workspace(m, n, k, rank, adapters, True)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    _launch(dev, lib.mixfp4_adapter_backward, _ptr(dy), lddy, _ptr(x), ldx, _ptr(t), _ptr(a),
+            _ptr(b), _ptr(scaling), _ptr(ranks), _ptr(plan.buf), _ptr(dx), lddx_in, m, n, k, rank,
+            adapters, p, _u64(seed), _u64(offset), _ptr(out), lddx, _ptr(da), _ptr(db), _ptr(ws),
+            need)
+    return out, da, db

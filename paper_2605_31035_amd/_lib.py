@@ -21,6 +21,8 @@ SYMBOLS = ("mixfp4_quantize_ws", "mixfp4_quantize_decode_ws",
            "mixfp4_decode_operand", "mixfp4_gemm_decoded", "mixfp4_gemm_noalloc",
            "mixfp4_gemm_noalloc_max_bytes", "mixfp4_decode_step",
            "mixfp4_quantize_variant", "mixfp4_dequantize_variant", "mixfp4_quantize_decode",
+           "mixfp4_dropout", "mixfp4_adapter_plan_bytes", "mixfp4_adapter_plan",
+           "mixfp4_adapter_workspace_size", "mixfp4_adapter", "mixfp4_adapter_backward",
            "mixfp4_status_string", "mixfp4_last_launch_error", "mixfp4_abi_version")
 
 
@@ -79,6 +81,23 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     h.mixfp4_quantize_decode.restype = i32
     h.mixfp4_gemm_noalloc_max_bytes.argtypes = []
     h.mixfp4_gemm_noalloc_max_bytes.restype = i64
+    f64 = ctypes.c_double
+    h.mixfp4_dropout.argtypes = [vp, i32, i64, vp, i32, i64, vp, i32, i64, i64, i64, f64, u64, u64,
+                                 vp]
+    h.mixfp4_dropout.restype = i32
+    h.mixfp4_adapter_plan_bytes.argtypes = [i64, i64, ctypes.POINTER(i64)]
+    h.mixfp4_adapter_plan_bytes.restype = i32
+    h.mixfp4_adapter_plan.argtypes = [vp, i64, i64, vp, i64, vp]
+    h.mixfp4_adapter_plan.restype = i32
+    h.mixfp4_adapter_workspace_size.argtypes = [i64] * 5 + [ctypes.POINTER(i64)] * 2
+    h.mixfp4_adapter_workspace_size.restype = i32
+    h.mixfp4_adapter.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, f64,
+                                 u64, u64, vp, vp, i32, i64, vp, i64, vp]
+    h.mixfp4_adapter.restype = i32
+    h.mixfp4_adapter_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, i64,
+                                          i64, i64, i64, i64, f64, u64, u64, vp, i64, vp, vp, vp,
+                                          i64, vp]
+    h.mixfp4_adapter_backward.restype = i32
     h.mixfp4_status_string.argtypes = [i32]
     h.mixfp4_status_string.restype = ctypes.c_char_p
     h.mixfp4_last_launch_error.argtypes = []

@@ -27,7 +27,8 @@ LIB = os.path.join(HERE, "libmixfp4.so")
 NATIVE = os.path.join(HERE, "_native.so")
 SOURCES = ["api.cpp", "quantize.hip", "quantize2d.hip", "dequantize.hip", "gemm.hip",
            "gemm_f16.hip", "gemm_direct.hip", "gemm_route.cpp", "decode_operand.hip",
-           "quantize_variant.hip"]
+           "quantize_variant.hip", "dropout.hip", "adapter_plan.hip", "adapter_shrink.hip",
+           "adapter_expand.hip", "adapter_grad.hip", "adapter_pass.cpp"]
 
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 HIPCC = os.path.join(ROCM, "bin", "hipcc")

@@ -1,0 +1,119 @@
+// Low-rank adapters beside a shared projection: shared pieces of the kernels.
+//
+// Row i of x has adapter l = index[i] (none outside [0, L)).  With rank
+// r_l <= R, A_l [R, K], B_l [n, R], scaling s_l, dropout's keep mask on x and
+// z = 1 / (1 - p):
+//   t_i  = z (keep_i x_i) A_l^T             out_i = c_i + s_l t_i B_l^T
+//   u_i  = s_l dy_i B_l                     dx_i  = dx0_i + z keep_i (u_i A_l)
+//   dA_l = z sum_i u_i^T (keep_i x_i)       dB_l  = s_l sum_i dy_i^T t_i
+// Every product runs on v_mfma_f32_16x16x32_bf16.  x, dy, A and B are bf16
+// and exact there.  t and u are fp32 sums; as operands they are carried as
+// bf16 terms.  Two terms in the products that a matrix is added to (out, dx):
+// |t - hi - lo| <= 2^-17 |t| (2^e <= |t|: a step of hi is 2^(e-7), the rest at
+// most 2^(e-8) and its own step below that 2^(e-16)), about 2^-19 in the mean.
+// Three in dA and dB, which stand alone: the rest of two is at most 2^(e-17),
+// so the third leaves 2^-26 |t|, less than t's own rounding.  With two the
+// gradients were 2.5e-6 from the exact ones, where fp32 operands give 3e-7
+// (333 rows) to 2e-6 (8192 rows).
+//
+// Rows are grouped by adapter into tiles of T rows (AdapterPlan): a position
+// is tile * T + row in the tile, and order[position] is the row of x or -1.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "internal.h"
+#include "philox.h"
+
+namespace mixfp4 {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ f32x4 mfma16(uint4 a, uint4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                 __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+__device__ __forceinline__ uint32_t bf16_bits(float v) {
+  return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v);
+}
+
+// v = hi + lo in bf16; an infinity or NaN stays whole in hi.
+__device__ __forceinline__ void split_bf16(float v, uint32_t& hi, uint32_t& lo) {
+  hi = bf16_bits(v);
+  const float h = __uint_as_float(hi << 16);
+  lo = (hi & 0x7F80u) == 0x7F80u ? 0u : bf16_bits(v - h);
+}
+
+// v = hi + mid + lo.
+__device__ __forceinline__ void split_bf16(float v, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+  split_bf16(v, hi, mid);
+  const float rest = (v - __uint_as_float(hi << 16)) - __uint_as_float(mid << 16);
+  lo = (hi & 0x7F80u) == 0x7F80u ? 0u : bf16_bits(rest);
+}
+
+// The keep bits of 8 consecutive elements from their group's draws: element e
+// takes the low (e even) or high half of word e / 2 and is kept from the
+// threshold on.  Returned as masks of the four words of packed bf16 pairs.
+__device__ __forceinline__ uint4 keep_masks(uint4 d, uint32_t threshold) {
+  const auto m = [&](uint32_t w) {
+    return ((w & 0xFFFFu) >= threshold ? 0xFFFFu : 0u) | ((w >> 16) >= threshold ? 0xFFFF0000u : 0u);
+  };
+  return make_uint4(m(d.x), m(d.y), m(d.z), m(d.w));
+}
+__device__ __forceinline__ uint4 and4(uint4 a, uint4 b) {
+  return make_uint4(a.x & b.x, a.y & b.y, a.z & b.z, a.w & b.w);
+}
+
+// 8 bf16 of a row from column `col` on; columns from `cols` on are zero and
+// not read.
+__device__ __forceinline__ uint4 load8(const uint16_t* row, int col, int cols) {
+  if (col + 8 <= cols) return *reinterpret_cast<const uint4*>(row + col);
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (col + e < cols) w[e >> 1] |= (uint32_t)row[col + e] << (16 * (e & 1));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// 8 bf16 with those from element `valid` on cleared.
+__device__ __forceinline__ uint4 clear_from(uint4 v, int valid) {
+  if (valid >= 8) return v;
+  const auto m = [&](uint32_t w, int e) {
+    return w & ((valid > e ? 0xFFFFu : 0u) | (valid > e + 1 ? 0xFFFF0000u : 0u));
+  };
+  return make_uint4(m(v.x, 0), m(v.y, 2), m(v.z, 4), m(v.w, 6));
+}
+
+// Transpose of 8 x 8 bf16: v[j] row j in, column c out in w[c].
+__device__ __forceinline__ void transpose8(const uint4 (&v)[8], uint4 (&w)[8]) {
+  const auto word = [](const uint4& q, int i) { return i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w; };
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    const uint32_t sel = (c & 1) ? 0x07060302u : 0x05040100u;   // high or low halves of two rows
+    w[c] = make_uint4(__builtin_amdgcn_perm(word(v[1], c >> 1), word(v[0], c >> 1), sel),
+                      __builtin_amdgcn_perm(word(v[3], c >> 1), word(v[2], c >> 1), sel),
+                      __builtin_amdgcn_perm(word(v[5], c >> 1), word(v[4], c >> 1), sel),
+                      __builtin_amdgcn_perm(word(v[7], c >> 1), word(v[6], c >> 1), sel));
+  }
+}
+
+// LDS tiles of rows of kSlots 16-byte slots: slot s of row r stands at
+// s ^ row_key(r), so that 8 consecutive rows at one slot (fragment reads) and
+// rows r, r + 8, ... at one slot (writes of transposed 8 x 8 blocks) fall
+// into different banks.
+__device__ __forceinline__ int row_key(int r) { return r ^ (r >> 3); }
+template <int kSlots>
+__device__ __forceinline__ int lds_slot(int row, int slot) {
+  return row * kSlots + (slot ^ (row_key(row) & (kSlots - 1)));
+}
+
+__device__ __forceinline__ int rank_of(const int32_t* ranks, int l, int rank) {
+  if (!ranks) return rank;
+  const int r = ranks[l];
+  return r < 0 ? 0 : r > rank ? rank : r;
+}
+
+}  // namespace mixfp4

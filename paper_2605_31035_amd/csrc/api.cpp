@@ -499,4 +499,141 @@ int mixfp4_gemm_decoded(const void* a_decoded, const float* a_tensor_scale,
       static_cast<const uint8_t*>(w_decoded), w_tensor_scale, m, n, k, c, s));
 }
 
+namespace {
+
+// threshold = p in 65536ths, to nearest; false where p is no probability.
+bool drop_params(double p, uint64_t seed, uint64_t offset, mixfp4::DropParams* d) {
+  if (!(p >= 0.0 && p <= 1.0)) return false;
+  d->key = {(uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)offset, (uint32_t)(offset >> 32)};
+  d->threshold = (uint32_t)__builtin_rint(p * 65536.0);
+  d->z = d->threshold == 65536u ? 0.0f : (float)(65536.0 / (65536.0 - d->threshold));
+  return true;
+}
+
+constexpr int64_t kMaxRows = int64_t(1) << 28, kMaxDim = int64_t(1) << 22;
+
+bool valid_groups(int64_t rows, int64_t adapters) {
+  return rows >= 0 && rows <= kMaxRows && adapters >= 1 && adapters <= mixfp4::kMaxAdapters;
+}
+
+bool valid_adapters(int64_t m, int64_t n, int64_t k, int64_t rank, int64_t adapters) {
+  return valid_groups(m, adapters) && n >= 1 && n <= kMaxDim && k >= 8 && k <= kMaxDim &&
+         k % 8 == 0 && rank >= 8 && rank <= mixfp4::kMaxRank && rank % 8 == 0;
+}
+
+bool valid_type(int32_t t) { return t == MIXFP4_TYPE_F32 || t == MIXFP4_TYPE_BF16; }
+uintptr_t type_bytes(int32_t t) { return t == MIXFP4_TYPE_BF16 ? 2 : 4; }
+
+}  // namespace
+
+int mixfp4_dropout(const void* x, int32_t x_type, int64_t ldx, const void* residual,
+                   int32_t residual_type, int64_t ldr, void* out, int32_t out_type, int64_t ldo,
+                   int64_t rows, int64_t k, double p, uint64_t seed, uint64_t offset,
+                   void* stream) {
+  if (!valid_type(x_type) || !valid_type(out_type) || (residual && !valid_type(residual_type)))
+    return MIXFP4_ERR_FLAGS;
+  mixfp4::DropoutArgs a{};
+  if (rows < 0 || k < 0 || k > (int64_t(1) << 32) || !drop_params(p, seed, offset, &a.drop))
+    return MIXFP4_ERR_SHAPE;
+  if (rows == 0 || k == 0) return MIXFP4_OK;
+  if (ldx < k || ldo < k || (residual && ldr < k)) return MIXFP4_ERR_SHAPE;
+  if (!x || !out) return MIXFP4_ERR_NULL;
+  if (!aligned(x, type_bytes(x_type)) || !aligned(out, type_bytes(out_type)) ||
+      (residual && !aligned(residual, type_bytes(residual_type))))
+    return MIXFP4_ERR_ALIGN;
+  a.x = x, a.residual = residual, a.out = out;
+  a.rows = rows, a.k = k, a.ldx = ldx, a.ldr = ldr, a.ldo = ldo;
+  a.x16 = x_type == MIXFP4_TYPE_BF16;
+  a.residual16 = residual_type == MIXFP4_TYPE_BF16;
+  a.out16 = out_type == MIXFP4_TYPE_BF16;
+  (void)hipGetLastError();
+  return launch_status(mixfp4::launch_dropout(a, static_cast<hipStream_t>(stream)));
+}
+
+int mixfp4_adapter_plan_bytes(int64_t rows, int64_t adapters, int64_t* bytes) {
+  if (!valid_groups(rows, adapters)) return MIXFP4_ERR_SHAPE;
+  if (!bytes) return MIXFP4_ERR_NULL;
+  *bytes = mixfp4::adapter_plan_bytes(rows, adapters);
+  return MIXFP4_OK;
+}
+
+int mixfp4_adapter_plan(const int32_t* index, int64_t rows, int64_t adapters, void* plan,
+                        int64_t plan_bytes, void* stream) {
+  if (!valid_groups(rows, adapters)) return MIXFP4_ERR_SHAPE;
+  if (!plan || (rows > 0 && !index)) return MIXFP4_ERR_NULL;
+  if (plan_bytes < mixfp4::adapter_plan_bytes(rows, adapters)) return MIXFP4_ERR_SHAPE;
+  if (!aligned(plan, 16) || !aligned(index, 4)) return MIXFP4_ERR_ALIGN;
+  (void)hipGetLastError();
+  return launch_status(mixfp4::launch_adapter_plan(index, rows, adapters, plan,
+                                                   static_cast<hipStream_t>(stream)));
+}
+
+int mixfp4_adapter_workspace_size(int64_t m, int64_t n, int64_t k, int64_t rank, int64_t adapters,
+                                  int64_t* forward_bytes, int64_t* backward_bytes) {
+  if (!valid_adapters(m, n, k, rank, adapters)) return MIXFP4_ERR_SHAPE;
+  if (!forward_bytes && !backward_bytes) return MIXFP4_ERR_NULL;
+  if (forward_bytes) *forward_bytes = mixfp4::adapter_workspace(m, n, k, rank, adapters, false);
+  if (backward_bytes) *backward_bytes = mixfp4::adapter_workspace(m, n, k, rank, adapters, true);
+  return MIXFP4_OK;
+}
+
+int mixfp4_adapter(const uint16_t* x, int64_t ldx, const uint16_t* a, const uint16_t* b,
+                   const float* scaling, const int32_t* ranks, const void* plan, const float* c,
+                   int64_t ldc, int64_t m, int64_t n, int64_t k, int64_t rank, int64_t adapters,
+                   double p, uint64_t seed, uint64_t offset, float* t, void* out, int32_t out_type,
+                   int64_t ldo, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!valid_type(out_type)) return MIXFP4_ERR_FLAGS;
+  mixfp4::AdapterArgs q{};
+  if (!valid_adapters(m, n, k, rank, adapters) || !drop_params(p, seed, offset, &q.drop))
+    return MIXFP4_ERR_SHAPE;
+  if (m == 0) return MIXFP4_OK;
+  if (ldx < k || ldx % 8 != 0 || (c && ldc < n) || ldo < n) return MIXFP4_ERR_SHAPE;
+  if (!x || !a || !b || !plan || !out || !workspace) return MIXFP4_ERR_NULL;
+  if (workspace_bytes < mixfp4::adapter_workspace(m, n, k, rank, adapters, false))
+    return MIXFP4_ERR_SHAPE;
+  if (!aligned(x, 16) || !aligned(a, 16) || !aligned(b, 16) || !aligned(plan, 16) ||
+      !aligned(scaling, 4) || !aligned(ranks, 4) || !aligned(c, 4) || !aligned(t, 4) ||
+      !aligned(out, type_bytes(out_type)) || !aligned(workspace, 256))
+    return MIXFP4_ERR_ALIGN;
+  q.m = m, q.n = n, q.k = k, q.rank = rank, q.adapters = adapters;
+  q.x = x, q.ldx = ldx, q.a = a, q.b = b, q.scaling = scaling, q.ranks = ranks;
+  q.plan = mixfp4::adapter_plan_at(const_cast<void*>(plan), m, adapters);
+  q.workspace = workspace;
+  q.c = c, q.ldc = ldc, q.out = out, q.ldo = ldo, q.out16 = out_type == MIXFP4_TYPE_BF16, q.t = t;
+  (void)hipGetLastError();
+  return launch_status(mixfp4::launch_adapter(q, static_cast<hipStream_t>(stream)));
+}
+
+int mixfp4_adapter_backward(const uint16_t* dy, int64_t lddy, const uint16_t* x, int64_t ldx,
+                            const float* t, const uint16_t* a, const uint16_t* b,
+                            const float* scaling, const int32_t* ranks, const void* plan,
+                            const float* dx_in, int64_t lddx_in, int64_t m, int64_t n, int64_t k,
+                            int64_t rank, int64_t adapters, double p, uint64_t seed,
+                            uint64_t offset, float* dx, int64_t lddx, float* da, float* db,
+                            void* workspace, int64_t workspace_bytes, void* stream) {
+  mixfp4::AdapterArgs q{};
+  if (!valid_adapters(m, n, k, rank, adapters) || !drop_params(p, seed, offset, &q.drop))
+    return MIXFP4_ERR_SHAPE;
+  if (m > 0 && (ldx < k || ldx % 8 != 0 || lddy < n || lddy % 8 != 0 || (dx_in && lddx_in < k) ||
+                lddx < k))
+    return MIXFP4_ERR_SHAPE;
+  if (!plan || !da || !db || !workspace) return MIXFP4_ERR_NULL;
+  if (m > 0 && (!dy || !x || !t || !a || !b || !dx)) return MIXFP4_ERR_NULL;
+  if (workspace_bytes < mixfp4::adapter_workspace(m, n, k, rank, adapters, true))
+    return MIXFP4_ERR_SHAPE;
+  if (!aligned(dy, 16) || !aligned(x, 16) || !aligned(a, 16) || !aligned(b, 16) ||
+      !aligned(plan, 16) || !aligned(scaling, 4) || !aligned(ranks, 4) || !aligned(t, 4) ||
+      !aligned(dx_in, 4) || !aligned(dx, 4) || !aligned(da, 16) || !aligned(db, 16) ||
+      !aligned(workspace, 256))
+    return MIXFP4_ERR_ALIGN;
+  q.m = m, q.n = n, q.k = k, q.rank = rank, q.adapters = adapters;
+  q.x = x, q.ldx = ldx, q.a = a, q.b = b, q.scaling = scaling, q.ranks = ranks;
+  q.plan = mixfp4::adapter_plan_at(const_cast<void*>(plan), m, adapters);
+  q.workspace = workspace;
+  q.t = const_cast<float*>(t), q.dy = dy, q.lddy = lddy;
+  q.dx0 = dx_in, q.lddx0 = lddx_in, q.dx = dx, q.lddx = lddx, q.da = da, q.db = db;
+  (void)hipGetLastError();
+  return launch_status(mixfp4::launch_adapter_backward(q, static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

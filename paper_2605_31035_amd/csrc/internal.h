@@ -238,4 +238,143 @@ hipError_t launch_dequantize_variant(const uint8_t* codes, const uint8_t* scales
 constexpr int64_t kStaticScratchBytes = int64_t(64) << 20;
 hipError_t static_scratch(void** ptr);
 
+// Dropout's draws: kept from the threshold (0 .. 65536) on, times z.
+struct DropParams {
+  SrParams key;
+  uint32_t threshold;
+  float z;               // 65536 / (65536 - threshold), 0 where nothing is kept
+};
+struct DropoutArgs {
+  const void* x;
+  const void* residual;  // NULL: none
+  void* out;
+  int64_t rows, k, ldx, ldr, ldo;
+  bool x16, residual16, out16;   // bf16 or fp32
+  DropParams drop;
+};
+hipError_t launch_dropout(const DropoutArgs& a, hipStream_t stream);
+
+// Rows grouped by adapter.  Tile i holds adapter_tile_rows positions; adapter
+// l has tiles seg[l] .. seg[l + 1], and l = adapters stands for the rows
+// without one.
+struct AdapterPlan {
+  int32_t* seg;            // adapters + 2
+  int32_t* tile_adapter;   // adapter_tiles_max; -1 for tiles not in use
+  int32_t* order;          // position -> row, or -1
+};
+constexpr int64_t kMaxAdapters = 4096, kMaxRank = 256;
+int adapter_tile_rows(int64_t rows, int64_t adapters);
+int64_t adapter_tiles_max(int64_t rows, int64_t adapters);
+int64_t adapter_plan_bytes(int64_t rows, int64_t adapters);
+AdapterPlan adapter_plan_at(void* p, int64_t rows, int64_t adapters);
+hipError_t launch_adapter_plan(const int32_t* index, int64_t rows, int64_t adapters, void* plan,
+                               hipStream_t stream);
+
+// One pass of the adapters (checked by the ABI layer); shapes in adapter.h.
+struct AdapterArgs {
+  int64_t m, n, k, rank, adapters;
+  const uint16_t* x;
+  int64_t ldx;
+  const uint16_t* a;
+  const uint16_t* b;
+  const float* scaling;    // NULL: 1
+  const int32_t* ranks;    // NULL: rank
+  AdapterPlan plan;
+  DropParams drop;
+  void* workspace;
+  // forward
+  const float* c;          // NULL: zero
+  int64_t ldc;
+  void* out;
+  int64_t ldo;
+  bool out16;
+  float* t;                // forward: written unless NULL; backward: read
+  // backward
+  const uint16_t* dy;
+  int64_t lddy;
+  const float* dx0;        // NULL: zero
+  int64_t lddx0;
+  float* dx;
+  int64_t lddx;
+  float* da;
+  float* db;
+};
+int64_t adapter_workspace(int64_t m, int64_t n, int64_t k, int64_t rank, int64_t adapters,
+                          bool backward);
+hipError_t launch_adapter(const AdapterArgs& a, hipStream_t stream);
+hipError_t launch_adapter_backward(const AdapterArgs& a, hipStream_t stream);
+
+// The pieces of a pass.  The padded rank is the matrix tiles' (16, 32, 64,
+// 128, 256); positions = tiles * tile rows.
+inline int padded_rank(int64_t rank) {
+  return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : rank <= 128 ? 128 : 256;
+}
+// part[s][position][rank] = the s-th of `splits` pieces of src W^T over the
+// contraction, W = A_l [rank, depth] (forward) or B_l^T, B_l [depth, rank].
+struct ShrinkArgs {
+  const uint16_t* src;
+  int64_t ld;
+  const uint16_t* w;
+  const int32_t* ranks;
+  AdapterPlan plan;
+  DropParams drop;         // threshold 0: none
+  int depth, rank, adapters, splits;
+  int64_t positions;
+  float* part;
+};
+hipError_t launch_adapter_shrink(const ShrinkArgs& a, int tile_rows, int64_t tiles, bool transposed,
+                                 hipStream_t stream);
+int adapter_shrink_splits(int64_t tiles, int64_t depth, int64_t rank);
+// Sums of the pieces times the factor s_l z: as two bf16 terms [position][2]
+// [max(32, padded)] and, unless NULL, as three [3][padded][positions];
+// the forward pass's t = z sum by rows, unless NULL.  With t_in, its rows
+// times s_l as transposed terms.
+struct JoinArgs {
+  const float* part;
+  const float* scaling;
+  const int32_t* ranks;
+  AdapterPlan plan;
+  int64_t positions;
+  int rank, adapters, splits;
+  float z;
+  uint16_t* terms;
+  uint16_t* terms_t;
+  float* t;
+  const float* t_in;
+  uint16_t* t_in_t;
+};
+hipError_t launch_adapter_join(const JoinArgs& a, int tile_rows, hipStream_t stream);
+// out = base + terms W^T, W = B_l [cols, rank] or (dx) A_l^T, A_l [rank, cols],
+// there with dropout's mask on the product.
+struct ExpandArgs {
+  const uint16_t* terms;
+  const uint16_t* w;
+  const int32_t* ranks;
+  AdapterPlan plan;
+  DropParams drop;
+  const float* base;
+  int64_t ldb;
+  void* out;
+  int64_t ldo;
+  int cols, rank, adapters;
+};
+hipError_t launch_adapter_expand(const ExpandArgs& a, int tile_rows, int64_t tiles, bool dx,
+                                 bool out16, hipStream_t stream);
+// dA_l [rank, cols] (src = x with dropout, terms of u) or dB_l [cols, rank]
+// (src = dy, terms of t), the positions in `splits` pieces whose partial sums
+// are joined.
+struct GradArgs {
+  const uint16_t* src;
+  int64_t ld;
+  const uint16_t* terms_t;
+  AdapterPlan plan;
+  DropParams drop;
+  int64_t positions;
+  int cols, rank, adapters, splits, tile_rows;
+  float* part;             // [2 splits][rank * cols]
+  float* out;
+};
+int adapter_grad_splits(int64_t m, int64_t cols, int64_t rank);
+hipError_t launch_adapter_grad(const GradArgs& a, bool db, hipStream_t stream);
+
 }  // namespace mixfp4
