@@ -685,6 +685,11 @@ def mixfp4_dropout(x: torch.Tensor, residual: torch.Tensor | None = None, p: flo
     any row pitch; ``out_dtype`` (default: x's) the result's type.  ``out`` may
     be x or residual itself.  The gradient of x is
     ``mixfp4_dropout(dy, p=p, seed=seed, offset=offset)``."""
+    if out is None and (out_dtype is None or out_dtype in _TYPES):
+        r = native.dropout(x, residual, p, seed, offset,
+                           None if out_dtype is None else out_dtype is torch.bfloat16)
+        if r is not None:
+            return r
     p = _probability(p)
     if out is not None:
         if out_dtype is not None and isinstance(out, torch.Tensor) and out.dtype != out_dtype:
@@ -723,6 +728,9 @@ def mixfp4_adapter_plan(index: torch.Tensor, adapters: int) -> AdapterPlan:
     i's adapter, or anything outside [0, adapters) for none.  The plan serves
     any number of calls on these rows (every adapted projection of the
     batch)."""
+    buf = native.adapter_plan(index, adapters)
+    if buf is not None:
+        return AdapterPlan(buf, index.shape[0], int(adapters))
     if not isinstance(index, torch.Tensor) or index.dim() != 1:
         raise ValueError("index must be a 1-D int32 tensor")
     m, adapters = index.shape[0], int(adapters)
@@ -788,6 +796,11 @@ def mixfp4_adapter(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, plan: Adap
     bfloat16; ``out`` may be c itself.  Rows without an adapter get c.
     Returns out [m, n], with ``keep_t`` (out, t): t fp32 [m, rank], what the
     backward pass needs of this one."""
+    if out is None and (out_dtype is None or out_dtype in _TYPES):
+        r = native.adapter(x, a, b, plan, c, scaling, ranks, p, seed, offset,
+                           out_dtype is torch.bfloat16, bool(keep_t))
+        if r is not None:
+            return r
     p = _probability(p)
     if out_dtype is not None and out_dtype not in _TYPES:
         raise ValueError("out_dtype must be torch.float32 or torch.bfloat16")
@@ -832,6 +845,10 @@ def mixfp4_adapter_backward(dy: torch.Tensor, x: torch.Tensor, t: torch.Tensor, 
     call and ``t`` what it kept; ``dx`` fp32 [m, k] the shared projection's own
     input gradient (DGRAD's result) or None for zero; ``out`` where the new one
     goes, which may be ``dx`` itself."""
+    if out is None:
+        r = native.adapter_backward(dy, x, t, a, b, plan, dx, scaling, ranks, p, seed, offset)
+        if r is not None:
+            return r
     p = _probability(p)
     if not isinstance(x, torch.Tensor) or x.dim() != 2:
         raise ValueError("x must be a 2-D tensor")

@@ -146,9 +146,18 @@ void launch(const ShrinkArgs& a, int64_t tiles, hipStream_t stream) {
 }
 
 // 16 positions per workgroup (they are of one adapter).  Mode 0 sums the
-// pieces, mode 1 takes t_in's rows.
-__global__ __launch_bounds__(kThreads) void join_kernel(JoinArgs a, int tile_rows, int padded) {
-  __shared__ float v[16][256 + 1];
+// pieces, mode 1 takes t_in's rows.  A thread sums four consecutive values;
+// with a small rank, several threads share the pieces and their sums are
+// added in a fixed order.  Pieces are read eight at a time, so that their
+// latencies overlap.
+template <int kRank>
+__global__ __launch_bounds__(kThreads) void join_kernel(JoinArgs a, int tile_rows) {
+  constexpr int kItems = 16 * kRank / 4;                    // float4 of the 16 positions
+  constexpr int kShare = kItems < kThreads ? kThreads / kItems : 1;
+  constexpr int kWide = kRank < 32 ? 32 : kRank;
+  constexpr int kPitch = kRank + 4;
+  __shared__ float v[16 * kPitch];
+  __shared__ f32x4 shared[kShare > 1 ? kThreads : 1];
   const int64_t p0 = (int64_t)blockIdx.x * 16;
   const int mode = blockIdx.y;
   const int l = a.plan.tile_adapter[p0 / tile_rows];
@@ -157,44 +166,76 @@ __global__ __launch_bounds__(kThreads) void join_kernel(JoinArgs a, int tile_row
   const bool none = l >= a.adapters;
   const int rank = none ? 0 : rank_of(a.ranks, l, a.rank);
   const float s = none || !a.scaling ? 1.0f : a.scaling[l];
-  for (int i = tid; i < 16 * padded; i += kThreads) {
-    const int q = i / padded, r = i % padded;
+  const int64_t piece = a.positions * a.rank;
+  for (int i = tid; i < kItems * kShare; i += kThreads) {
+    const int item = i % kItems, part = i / kItems;
+    const int q = item / (kRank / 4), r = item % (kRank / 4) * 4;
     const int row = a.plan.order[p0 + q];
-    float sum = 0.0f;
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
     if (r < rank && row >= 0) {
       if (mode == 1) {
-        sum = a.t_in[(int64_t)row * a.rank + r];
+        if (part == 0) {
+          const float* t = a.t_in + (int64_t)row * a.rank + r;   // any 4-byte alignment
+          sum = f32x4{t[0], t[1], t[2], t[3]};
+        }
       } else {
-        const float* part = a.part + (p0 + q) * a.rank + r;
-        for (int j = 0; j < a.splits; ++j) sum += part[(int64_t)j * a.positions * a.rank];
-        sum *= a.z;
+        const float* from = a.part + (p0 + q) * a.rank + r;
+        int j = part;
+        for (; j + 7 * kShare < a.splits; j += 8 * kShare) {
+          f32x4 u[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            u[e] = *reinterpret_cast<const f32x4*>(from + (j + e * kShare) * piece);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum += u[e];
+        }
+        for (; j < a.splits; j += kShare) sum += *reinterpret_cast<const f32x4*>(from + j * piece);
       }
     }
-    if (mode == 0 && a.t && row >= 0 && r < a.rank) a.t[(int64_t)row * a.rank + r] = sum;
-    v[q][r] = s * sum;
+    if constexpr (kShare > 1) {
+      shared[tid] = sum;
+      __syncthreads();                                     // one round: kItems * kShare threads
+      if (part > 0) break;
+#pragma unroll
+      for (int e = 1; e < kShare; ++e) sum += shared[tid + e * kItems];
+    }
+    if (mode == 0) sum *= a.z;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (r + e >= rank) sum[e] = 0.0f;
+    if (mode == 0 && a.t && row >= 0 && r < a.rank) {
+      float* t = a.t + (int64_t)row * a.rank + r;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t[e] = sum[e];
+    }
+    *reinterpret_cast<f32x4*>(&v[q * kPitch + r]) = s * sum;
   }
   if (none) return;
   __syncthreads();
-  if (mode == 0 && a.terms) {
-    const int width = padded < 32 ? 32 : padded;
-    for (int i = tid; i < 16 * width; i += kThreads) {
-      const int q = i / width, r = i % width;
-      uint32_t hi = 0u, lo = 0u;
-      if (r < padded) split_bf16(v[q][r], hi, lo);
-      uint16_t* to = a.terms + (p0 + q) * 2 * width + r;
-      to[0] = (uint16_t)hi;
-      to[width] = (uint16_t)lo;
+  if (mode == 0) {
+    for (int i = tid; i < 16 * kWide / 2; i += kThreads) {
+      const int q = i / (kWide / 2), r = i % (kWide / 2) * 2;
+      uint32_t hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
+      if (r < kRank) {
+        split_bf16(v[q * kPitch + r], hi[0], lo[0]);
+        split_bf16(v[q * kPitch + r + 1], hi[1], lo[1]);
+      }
+      uint32_t* to = reinterpret_cast<uint32_t*>(a.terms + (p0 + q) * 2 * kWide + r);
+      to[0] = hi[0] | hi[1] << 16;
+      to[kWide / 2] = lo[0] | lo[1] << 16;
     }
   }
   uint16_t* transposed = mode == 0 ? a.terms_t : a.t_in_t;
   if (transposed)
-    for (int i = tid; i < 16 * padded; i += kThreads) {
-      const int q = i % 16, r = i / 16;
-      uint32_t part[3];
-      split_bf16(v[q][r], part[0], part[1], part[2]);
+    for (int i = tid; i < 8 * kRank; i += kThreads) {
+      const int q = i % 8 * 2, r = i / 8;
+      uint32_t x[3], y[3];
+      split_bf16(v[q * kPitch + r], x[0], x[1], x[2]);
+      split_bf16(v[(q + 1) * kPitch + r], y[0], y[1], y[2]);
 #pragma unroll
       for (int h = 0; h < 3; ++h)
-        transposed[((int64_t)h * padded + r) * a.positions + p0 + q] = (uint16_t)part[h];
+        *reinterpret_cast<uint32_t*>(transposed + ((int64_t)h * kRank + r) * a.positions + p0 + q) =
+            x[h] | y[h] << 16;
     }
 }
 
@@ -220,8 +261,14 @@ hipError_t launch_adapter_shrink(const ShrinkArgs& a, int tile_rows, int64_t til
 }
 
 hipError_t launch_adapter_join(const JoinArgs& a, int tile_rows, hipStream_t stream) {
-  join_kernel<<<dim3((unsigned)(a.positions / 16), a.t_in ? 2 : 1), kThreads, 0, stream>>>(
-      a, tile_rows, padded_rank(a.rank));
+  const dim3 grid((unsigned)(a.positions / 16), a.t_in ? 2 : 1);
+  switch (padded_rank(a.rank)) {
+    case 16: join_kernel<16><<<grid, kThreads, 0, stream>>>(a, tile_rows); break;
+    case 32: join_kernel<32><<<grid, kThreads, 0, stream>>>(a, tile_rows); break;
+    case 64: join_kernel<64><<<grid, kThreads, 0, stream>>>(a, tile_rows); break;
+    case 128: join_kernel<128><<<grid, kThreads, 0, stream>>>(a, tile_rows); break;
+    default: join_kernel<256><<<grid, kThreads, 0, stream>>>(a, tile_rows); break;
+  }
   return hipGetLastError();
 }
 

@@ -291,7 +291,236 @@ PyObject* dequantize(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
+// The values of a matrix argument: address, pitch and whether bf16.
+struct Matrix {
+  void* p = nullptr;
+  int64_t rows = 0, cols = 0, pitch = 0;
+  bool half = false;
+  c10::Device device = c10::Device(c10::kCPU);
+};
+
+// An fp32 or bf16 matrix whose rows are contiguous and apart.
+bool matrix_arg(PyObject* o, bool allow_f32, bool allow_bf16, Matrix& m) {
+  const at::Tensor* t = allow_f32 ? plain(o, at::kFloat, 2) : nullptr;
+  if (!t && allow_bf16 && (t = plain(o, at::kBFloat16, 2))) m.half = true;
+  if (!t) return false;
+  m.rows = t->size(0);
+  m.cols = t->size(1);
+  if (m.rows <= 0 || m.cols <= 0 || (m.cols > 1 && t->stride(1) != 1)) return false;
+  m.pitch = m.rows > 1 ? t->stride(0) : (m.cols + 7) / 8 * 8;
+  if (m.pitch < m.cols) return false;
+  m.p = t->data_ptr();
+  m.device = t->device();
+  return true;
+}
+
+// None, or a contiguous vector of `n` elements.
+bool vector_arg(PyObject* o, at::ScalarType type, int64_t n, void** p) {
+  *p = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor* t = plain(o, type, 1);
+  if (!t || t->size(0) != n || !t->is_contiguous()) return false;
+  *p = t->data_ptr();
+  return true;
+}
+
+struct Draws {
+  double p;
+  uint64_t seed, offset;
+};
+bool draws_arg(PyObject* p, PyObject* seed, PyObject* offset, Draws& d) {
+  d.p = PyFloat_AsDouble(p);
+  if (!PyErr_Occurred()) d.seed = PyLong_AsUnsignedLongLongMask(seed);
+  if (!PyErr_Occurred()) d.offset = PyLong_AsUnsignedLongLongMask(offset);
+  if (PyErr_Occurred()) {
+    PyErr_Clear();
+    return false;
+  }
+  return true;
+}
+
+// dropout(x, residual, p, seed, offset, out16 or None)
+PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 6) Py_RETURN_NONE;
+  return guarded([&]() -> PyObject* {
+    Matrix x, r;
+    Draws d;
+    if (!matrix_arg(args[0], true, true, x) || !draws_arg(args[2], args[3], args[4], d)) return nullptr;
+    if (args[1] != Py_None &&
+        (!matrix_arg(args[1], true, true, r) || r.rows != x.rows || r.cols != x.cols))
+      return nullptr;
+    const bool half = args[5] == Py_None ? x.half : args[5] == Py_True;
+    at::Tensor out;
+    int st;
+    {
+      const WithoutGil released;
+      out = empty({x.rows, x.cols}, half ? at::kBFloat16 : at::kFloat, x.device);
+      st = mixfp4_dropout(x.p, x.half, x.pitch, r.p, r.half, r.pitch, out.data_ptr(), half, x.cols,
+                          x.rows, x.cols, d.p, d.seed, d.offset, stream_of(x.device));
+    }
+    return st == MIXFP4_OK ? THPVariable_Wrap(out) : nullptr;
+  });
+}
+
+// adapter_plan(index, adapters): the plan's buffer
+PyObject* adapter_plan(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 2) Py_RETURN_NONE;
+  return guarded([&]() -> PyObject* {
+    const at::Tensor* index = plain(args[0], at::kInt, 1);
+    if (!index || !index->is_contiguous() || index->size(0) <= 0) return nullptr;
+    const int64_t adapters = PyLong_AsLongLong(args[1]);
+    if (PyErr_Occurred()) {
+      PyErr_Clear();
+      return nullptr;
+    }
+    int64_t need = 0;
+    const int64_t rows = index->size(0);
+    if (mixfp4_adapter_plan_bytes(rows, adapters, &need) != MIXFP4_OK) return nullptr;
+    const int32_t* ip = static_cast<const int32_t*>(index->data_ptr());
+    const c10::Device dev = index->device();
+    at::Tensor plan;
+    int st;
+    {
+      const WithoutGil released;
+      plan = empty({need}, at::kByte, dev);
+      st = mixfp4_adapter_plan(ip, rows, adapters, plan.data_ptr(), need, stream_of(dev));
+    }
+    return st == MIXFP4_OK ? THPVariable_Wrap(plan) : nullptr;
+  });
+}
+
+// The operands that the adapters' passes share: x, a, b, plan (buffer, rows,
+// adapters), scaling, ranks, draws.
+struct Adapters {
+  Matrix x;
+  const uint16_t *a = nullptr, *b = nullptr;
+  void *plan = nullptr, *scaling = nullptr, *ranks = nullptr;
+  int64_t n = 0, rank = 0, count = 0;
+  Draws d{};
+};
+bool adapters_arg(PyObject* x, PyObject* a, PyObject* b, PyObject* plan, PyObject* scaling,
+                  PyObject* ranks, PyObject* p, PyObject* seed, PyObject* offset, Adapters& q) {
+  if (!matrix_arg(x, false, true, q.x)) return false;
+  const at::Tensor* at_ = plain(a, at::kBFloat16, 3);
+  const at::Tensor* bt = plain(b, at::kBFloat16, 3);
+  if (!at_ || !bt || !at_->is_contiguous() || !bt->is_contiguous()) return false;
+  q.count = at_->size(0);
+  q.rank = at_->size(1);
+  q.n = bt->size(1);
+  if (at_->size(2) != q.x.cols || bt->size(0) != q.count || bt->size(2) != q.rank) return false;
+  if (!PyTuple_Check(plan) || PyTuple_GET_SIZE(plan) != 3) return false;
+  const at::Tensor* buf = plain(PyTuple_GET_ITEM(plan, 0), at::kByte, 1);
+  const int64_t rows = PyLong_AsLongLong(PyTuple_GET_ITEM(plan, 1));
+  const int64_t count = PyLong_AsLongLong(PyTuple_GET_ITEM(plan, 2));
+  if (PyErr_Occurred()) {
+    PyErr_Clear();
+    return false;
+  }
+  int64_t need = 0;
+  if (!buf || !buf->is_contiguous() || rows != q.x.rows || count != q.count ||
+      mixfp4_adapter_plan_bytes(rows, count, &need) != MIXFP4_OK || buf->numel() != need)
+    return false;
+  q.plan = buf->data_ptr();
+  q.a = static_cast<const uint16_t*>(at_->data_ptr());
+  q.b = static_cast<const uint16_t*>(bt->data_ptr());
+  return vector_arg(scaling, at::kFloat, q.count, &q.scaling) &&
+         vector_arg(ranks, at::kInt, q.count, &q.ranks) && draws_arg(p, seed, offset, q.d);
+}
+
+// adapter(x, a, b, plan, c, scaling, ranks, p, seed, offset, out16, keep_t):
+// out, or (out, t)
+PyObject* adapter(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 12) Py_RETURN_NONE;
+  return guarded([&]() -> PyObject* {
+    Adapters q;
+    Matrix c;
+    if (!adapters_arg(args[0], args[1], args[2], args[3], args[5], args[6], args[7], args[8],
+                      args[9], q))
+      return nullptr;
+    if (args[4] != Py_None &&
+        (!matrix_arg(args[4], true, false, c) || c.rows != q.x.rows || c.cols != q.n))
+      return nullptr;
+    const bool half = args[10] == Py_True, keep = args[11] == Py_True;
+    int64_t need = 0;
+    if (mixfp4_adapter_workspace_size(q.x.rows, q.n, q.x.cols, q.rank, q.count, &need, nullptr) !=
+        MIXFP4_OK)
+      return nullptr;
+    const c10::Device dev = q.x.device;
+    at::Tensor out, t, ws;
+    int st;
+    {
+      const WithoutGil released;
+      out = empty({q.x.rows, q.n}, half ? at::kBFloat16 : at::kFloat, dev);
+      if (keep) t = empty({q.x.rows, q.rank}, at::kFloat, dev);
+      ws = empty({need}, at::kByte, dev);
+      st = mixfp4_adapter(static_cast<const uint16_t*>(q.x.p), q.x.pitch, q.a, q.b,
+                          static_cast<const float*>(q.scaling), static_cast<const int32_t*>(q.ranks),
+                          q.plan, static_cast<const float*>(c.p), c.pitch, q.x.rows, q.n, q.x.cols,
+                          q.rank, q.count, q.d.p, q.d.seed, q.d.offset,
+                          keep ? floats(t) : nullptr, out.data_ptr(), half, q.n, ws.data_ptr(), need,
+                          stream_of(dev));
+    }
+    if (st != MIXFP4_OK) return nullptr;
+    if (!keep) return THPVariable_Wrap(out);
+    PyObject* o = THPVariable_Wrap(out);
+    PyObject* u = THPVariable_Wrap(t);
+    PyObject* r = PyTuple_Pack(2, o, u);
+    Py_DECREF(o);
+    Py_DECREF(u);
+    return r;
+  });
+}
+
+// adapter_backward(dy, x, t, a, b, plan, dx, scaling, ranks, p, seed, offset):
+// (dx, da, db)
+PyObject* adapter_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 12) Py_RETURN_NONE;
+  return guarded([&]() -> PyObject* {
+    Adapters q;
+    Matrix dy, dx0;
+    if (!adapters_arg(args[1], args[3], args[4], args[5], args[7], args[8], args[9], args[10],
+                      args[11], q))
+      return nullptr;
+    const int64_t m = q.x.rows, k = q.x.cols;
+    if (!matrix_arg(args[0], false, true, dy) || dy.rows != m || dy.cols != q.n) return nullptr;
+    const at::Tensor* t = matrix(args[2], at::kFloat, m, q.rank);
+    if (!t) return nullptr;
+    if (args[6] != Py_None &&
+        (!matrix_arg(args[6], true, false, dx0) || dx0.rows != m || dx0.cols != k))
+      return nullptr;
+    int64_t need = 0;
+    if (mixfp4_adapter_workspace_size(m, q.n, k, q.rank, q.count, nullptr, &need) != MIXFP4_OK)
+      return nullptr;
+    const float* tp = floats(*t);
+    const c10::Device dev = q.x.device;
+    at::Tensor dx, da, db, ws;
+    int st;
+    {
+      const WithoutGil released;
+      dx = empty({m, k}, at::kFloat, dev);
+      da = empty({q.count, q.rank, k}, at::kFloat, dev);
+      db = empty({q.count, q.n, q.rank}, at::kFloat, dev);
+      ws = empty({need}, at::kByte, dev);
+      st = mixfp4_adapter_backward(
+          static_cast<const uint16_t*>(dy.p), dy.pitch, static_cast<const uint16_t*>(q.x.p),
+          q.x.pitch, tp, q.a, q.b, static_cast<const float*>(q.scaling),
+          static_cast<const int32_t*>(q.ranks), q.plan, static_cast<const float*>(dx0.p), dx0.pitch,
+          m, q.n, k, q.rank, q.count, q.d.p, q.d.seed, q.d.offset, floats(dx), k, floats(da),
+          floats(db), ws.data_ptr(), need, stream_of(dev));
+    }
+    if (st != MIXFP4_OK) return nullptr;
+    PyObject* z = THPVariable_Wrap(db);
+    PyObject* r = triple(dx, da, z);
+    Py_DECREF(z);
+    return r;
+  });
+}
+
 PyMethodDef kMethods[] = {
+    {"dropout", reinterpret_cast<PyCFunction>(dropout), METH_FASTCALL, nullptr},
+    {"adapter_plan", reinterpret_cast<PyCFunction>(adapter_plan), METH_FASTCALL, nullptr},
+    {"adapter", reinterpret_cast<PyCFunction>(adapter), METH_FASTCALL, nullptr},
+    {"adapter_backward", reinterpret_cast<PyCFunction>(adapter_backward), METH_FASTCALL, nullptr},
     {"quantize", reinterpret_cast<PyCFunction>(quantize), METH_FASTCALL, nullptr},
     {"gemm", reinterpret_cast<PyCFunction>(gemm), METH_FASTCALL, nullptr},
     {"decode_step", reinterpret_cast<PyCFunction>(decode_step), METH_FASTCALL, nullptr},
