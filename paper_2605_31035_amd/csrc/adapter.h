@@ -100,6 +100,19 @@ __device__ __forceinline__ void transpose8(const uint4 (&v)[8], uint4 (&w)[8]) {
   }
 }
 
+// Transpose of 8 rows of 4 bf16: column c out in w[c].
+__device__ __forceinline__ void transpose8x4(const uint2 (&v)[8], uint4 (&w)[4]) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const uint32_t sel = (c & 1) ? 0x07060302u : 0x05040100u;
+    const auto word = [&](int j) { return c < 2 ? v[j].x : v[j].y; };
+    w[c] = make_uint4(__builtin_amdgcn_perm(word(1), word(0), sel),
+                      __builtin_amdgcn_perm(word(3), word(2), sel),
+                      __builtin_amdgcn_perm(word(5), word(4), sel),
+                      __builtin_amdgcn_perm(word(7), word(6), sel));
+  }
+}
+
 // LDS tiles of rows of kSlots 16-byte slots: slot s of row r stands at
 // s ^ row_key(r), so that 8 consecutive rows at one slot (fragment reads) and
 // rows r, r + 8, ... at one slot (writes of transposed 8 x 8 blocks) fall
@@ -114,6 +127,15 @@ __device__ __forceinline__ int rank_of(const int32_t* ranks, int l, int rank) {
   if (!ranks) return rank;
   const int r = ranks[l];
   return r < 0 ? 0 : r > rank ? rank : r;
+}
+
+// A grid of `across` workgroups per tile, those of one tile side by side: the
+// rows of a matrix often lie a multiple of some KB apart, and workgroups that
+// read all rows at the same columns at the same time meet in few memory
+// channels.
+inline dim3 tile_grid(int64_t across, int64_t tiles) {
+  const int64_t y = tiles < 32768 ? tiles : 32768;
+  return dim3((unsigned)across, (unsigned)y, (unsigned)((tiles + y - 1) / y));
 }
 
 }  // namespace mixfp4

@@ -8,167 +8,270 @@ namespace mixfp4 {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBlock32 = 32;   // columns of a wave's step
 
-// One workgroup: one tile of rows, `width` columns.  The terms of the tile
-// stand in LDS; a wave takes 32 columns at a time for all rows of the tile.
-// W is the left operand of the matrix instructions, so that a lane of the
-// result holds one row; of two instructions with columns 8 q + 0..3 and
-// 8 q + 4..7 it holds 8 consecutive columns: 32 bytes of fp32, and one group
-// of dropout's draws.
-template <int kT, int kRank, bool kDx, bool kOut16>
-__global__ __launch_bounds__(kThreads) void expand_kernel(ExpandArgs a, int width, bool aligned) {
+// One workgroup: one tile of rows, `width` columns, 128 at a time and 32 of
+// them per wave.  The terms of the tile stand in LDS.  W is the left operand
+// of the matrix instructions, so that a lane of the result holds one row; of
+// two instructions with columns 8 q + 0..3 and 8 q + 4..7 it holds 8
+// consecutive columns, one group of dropout's draws.  The wave then turns
+// its 16 x 32 results in LDS of its own, so that 8 lanes read the base and
+// write out of one row, a whole 128-byte line (kAligned; otherwise 32 lanes,
+// 4 bytes each).  What the next block needs from memory is requested before
+// this block is stored: loads behind stores wait for them.  Loads are made
+// without branches, from a row or column that is there in place of one that
+// is not; only tiles and blocks that are not full look at each store.
+template <int kT, int kRank, bool kDx, bool kOut16, bool kAligned>
+__global__ __launch_bounds__(kThreads) void expand_kernel(ExpandArgs a, int width, int tiles) {
   constexpr int kWide = kRank < 32 ? 32 : kRank;     // terms per part
   constexpr int kSteps = kWide / 32;
   constexpr int kRows = kT / 16;
-  constexpr int kPitch = 2 * kWide / 8 + 1;          // 16-byte units; odd against bank conflicts
   constexpr int kSlots = kWide / 8;
-  __shared__ uint4 terms[kT * kPitch];
-  __shared__ uint4 wt[kDx ? 128 * kSlots : 1];
-  const int tile = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  // pieces of W per thread and block: 16 bytes of B_l, or 8 rows by 4 columns
+  // of A_l
+  constexpr int kPieces = kDx ? (32 * kSlots + kThreads - 1) / kThreads : kWide / 16;
+  constexpr bool kAhead = kRank <= 128;              // registers for W of the next block
+  __shared__ uint4 terms[kT * 2 * kSlots];
+  __shared__ uint4 wt[128 * kSlots];
+  __shared__ f32x4 turn[4][16 * 8];
+  __shared__ int32_t order[kT];
+  const int tile = blockIdx.z * gridDim.y + blockIdx.y;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int r16 = lane & 15, g = lane >> 4;
+  if (tile >= tiles) return;
   const int l = a.plan.tile_adapter[tile];
   if (l < 0) return;
   const bool none = l >= a.adapters;
   const int rank = none ? 0 : rank_of(a.ranks, l, a.rank);
   const int64_t p0 = (int64_t)tile * kT;
-  if (rank > 0) {
-    const uint4* from = reinterpret_cast<const uint4*>(a.terms + p0 * 2 * kWide);
-    for (int i = tid; i < kT * (kPitch - 1); i += kThreads)
-      terms[i / (kPitch - 1) * kPitch + i % (kPitch - 1)] = from[i];
-    __syncthreads();
-  }
-  int rows[kRows];
-#pragma unroll
-  for (int i = 0; i < kRows; ++i) rows[i] = a.plan.order[p0 + i * 16 + r16];
   const uint16_t* w = a.w + (none ? 0 : (int64_t)l * a.rank * a.cols);
-  const int begin = blockIdx.y * width;
+  const int begin = blockIdx.x * width;
   const int end = a.cols - begin < width ? a.cols : begin + width;
 
-  for (int block = begin; block < end; block += 128) {
+  // pieces of 16 bytes of B_l: column and slot of each, the same in every block
+  const int slots = a.rank >> 3;
+  int piece_col[kDx ? 1 : kPieces], piece_at[kDx ? 1 : kPieces];
+  if constexpr (!kDx) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int p = lane + 64 * i, col = p / slots, slot = p - col * slots;
+      piece_col[i] = col < 32 ? col : 32;
+      piece_at[i] = col < 32 ? lds_slot<kSlots>(wave * 32 + col, slot) : 0;
+      if (slot * 8 >= rank) piece_col[i] |= 0x100;              // behind the adapter's rank
+      else if (slot * 8 + 8 > rank) piece_col[i] |= 0x200;
+    }
+  }
+  uint4 wf[kDx ? 1 : kPieces];
+  uint2 wp[kDx ? kPieces : 1][8];
+  const auto load_w = [&](int block) {
+    if (rank == 0) return;
     if constexpr (kDx) {
-      // A_l's columns block .. block + 128, transposed: [128][rank]
-      if (rank > 0) {
-        __syncthreads();
-        for (int p = tid; p < 16 * kSlots; p += kThreads) {
-          const int cb = p % 16, rb = p / 16;
-          const int col = block + cb * 8;
-          uint4 v[8], q[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            v[j] = rb * 8 + j < rank && col < end
-                       ? *reinterpret_cast<const uint4*>(w + (int64_t)(rb * 8 + j) * a.cols + col)
-                       : make_uint4(0, 0, 0, 0);
-          transpose8(v, q);
+      for (int i = 0; i < kPieces; ++i) {
+        const int p = tid + i * kThreads, cb = p % 32, rb = p / 32;
+        int col = block + cb * 4;
+        col = col < end ? col : end - 4;
 #pragma unroll
-          for (int c = 0; c < 8; ++c) wt[lds_slot<kSlots>(cb * 8 + c, rb)] = q[c];
+        for (int j = 0; j < 8; ++j) {
+          const int r = rb * 8 + j < rank ? rb * 8 + j : 0;
+          wp[i][j] = *reinterpret_cast<const uint2*>(w + (int64_t)r * a.cols + col);
         }
-        __syncthreads();
+      }
+    } else {
+      // 32 columns of B_l stand side by side
+      const int c0 = block + wave * 32;
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const int p = lane + 64 * i;
+        const bool there = (piece_col[i] & 0xFF) < 32 && c0 + (piece_col[i] & 0xFF) < end;
+        wf[i] = *reinterpret_cast<const uint4*>(w + (there ? (int64_t)c0 * a.rank + p * 8 : 0));
       }
     }
-    const int c0 = block + wave * kBlock32;
-    if (c0 >= end) continue;
-    f32x4 acc[kRows][2];
+  };
+  load_w(begin);
+
+  if (tid < kT) order[tid] = a.plan.order[p0 + tid];
+  if (rank > 0) {
+    const uint4* from = reinterpret_cast<const uint4*>(a.terms + p0 * 2 * kWide);
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) acc[i][0] = acc[i][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      if (s * 32 >= rank) break;
-      uint4 wf[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int col = 8 * (r16 >> 2) + 4 * j + (r16 & 3);
-        if constexpr (kDx) {
-          wf[j] = wt[lds_slot<kSlots>(wave * kBlock32 + col, 4 * s + g)];
-        } else {
-          const int r = 32 * s + 8 * g;
-          wf[j] = c0 + col < end && r < rank
-                      ? clear_from(*reinterpret_cast<const uint4*>(
-                                       w + (int64_t)(c0 + col) * a.rank + r), rank - r)
-                      : make_uint4(0, 0, 0, 0);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < kRows; ++i) {
-        const uint4 hi = terms[(i * 16 + r16) * kPitch + 4 * s + g];
-        const uint4 lo = terms[(i * 16 + r16) * kPitch + kSlots + 4 * s + g];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          acc[i][j] = mfma16(wf[j], lo, acc[i][j]);
-          acc[i][j] = mfma16(wf[j], hi, acc[i][j]);
-        }
-      }
+    for (int i = 0; i < (kT * 2 * kSlots + kThreads - 1) / kThreads; ++i) {
+      const int p = tid + i * kThreads;
+      if (p < kT * 2 * kSlots) terms[lds_slot<2 * kSlots>(p / (2 * kSlots), p % (2 * kSlots))] = from[p];
     }
-    const int col = c0 + 8 * g;
-    const int valid = end - col < 8 ? end - col : 8;
-    const bool wide = aligned && valid == 8;
+  }
+  if constexpr (!kDx) {
+    if (a.rank < kWide)                      // the rank padded to whole matrix steps
+      for (int p = tid; p < 128 * kSlots; p += kThreads)
+        if (p % kSlots >= slots) wt[lds_slot<kSlots>(p / kSlots, p % kSlots)] = make_uint4(0, 0, 0, 0);
+  }
+  __syncthreads();
+
+  // this lane's rows: of its loads and stores, those that are not there
+  // replaced by the tile's first for loads
+  constexpr int kLoads = kAligned ? 2 * kRows : 8 * kRows;
+  constexpr int kLanes = kAligned ? 8 : 32;
+  const int sub = lane / kLanes, lane_col = lane % kLanes * (kAligned ? 4 : 1);
+  const bool whole = order[kT - 1] >= 0;
+  const auto row_of = [&](int i) { return order[i * (64 / kLanes) + sub]; };
+  f32x4 base[kRows][2];
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) base[i][0] = base[i][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const auto load_base = [&](int block) {
+    if (!a.base) return;
+    int col = block + wave * 32 + lane_col;
+    col = col < end ? col : end - (kAligned ? 4 : 1);
+    const float* from = a.base + col;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      int row = row_of(i);
+      row = row < 0 ? order[0] : row;
+      const float* p = from + (uint64_t)(uint32_t)row * (uint32_t)a.ldb;
+      if constexpr (kAligned)
+        base[i >> 1][i & 1] = *reinterpret_cast<const f32x4*>(p);
+      else
+        base[i >> 3][(i >> 2) & 1][i & 3] = *p;
+    }
+  };
+  load_base(begin);
+
+  for (int block = begin; block < end; block += 128) {
+    const int c0 = block + wave * 32;
+    const bool more = block + 128 < end;
+    f32x4 acc[kRows][2], held[kRows][2];
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
-      if (rows[i] < 0 || valid <= 0) continue;
-      float v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = acc[i][e >> 2][e & 3];
+      acc[i][0] = acc[i][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      held[i][0] = base[i][0];
+      held[i][1] = base[i][1];
+    }
+    if (rank > 0) {
       if constexpr (kDx) {
-        if (a.drop.threshold) {
-          const uint4 d = block_draws((int64_t)rows[i] * (a.cols / 8) + col / 8, a.drop.key);
+        if (block > begin) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          const int p = tid + i * kThreads, cb = p % 32, rb = p / 32;
+          uint4 q[4];
+          if (rank < kWide) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (rb * 8 + j >= rank) wp[i][j] = make_uint2(0, 0);
+          }
+          transpose8x4(wp[i], q);
+          if (32 * kSlots % kThreads == 0 || rb < kSlots)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) wt[lds_slot<kSlots>(cb * 4 + c, rb)] = q[c];
+        }
+        __syncthreads();
+      } else {
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          uint4 v = wf[i];
+          if (rank < a.rank) {
+            if (piece_col[i] & 0x100) v = make_uint4(0, 0, 0, 0);
+            if (piece_col[i] & 0x200) v = clear_from(v, rank & 7);
+          }
+          if ((piece_col[i] & 0xFF) < 32) wt[piece_at[i]] = v;
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+      if (kAhead && more) load_w(block + 128);
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        if (s * 32 >= rank) break;
+        uint4 f[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          f[j] = wt[lds_slot<kSlots>(wave * 32 + 8 * (r16 >> 2) + 4 * j + (r16 & 3), 4 * s + g)];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+          const uint4 hi = terms[lds_slot<2 * kSlots>(i * 16 + r16, 4 * s + g)];
+          const uint4 lo = terms[lds_slot<2 * kSlots>(i * 16 + r16, kSlots + 4 * s + g)];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            acc[i][j] = mfma16(f[j], lo, acc[i][j]);
+            acc[i][j] = mfma16(f[j], hi, acc[i][j]);
+          }
+        }
+      }
+    }
+    if (more) {
+      if (!kAhead) load_w(block + 128);
+      load_base(block + 128);
+    }
+    if constexpr (kDx) {
+      if (a.drop.threshold) {
+        const int col = c0 + 8 * g;
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+          const int row = order[i * 16 + r16];
+          const uint4 d = block_draws((int64_t)row * (a.cols / 8) + col / 8, a.drop.key);
           const uint32_t u[4] = {d.x, d.y, d.z, d.w};
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if ((e & 1 ? u[e >> 1] >> 16 : u[e >> 1] & 0xFFFFu) < a.drop.threshold) v[e] = 0.0f;
-        }
-      }
-      if (a.base) {
-        const float* base = a.base + (int64_t)rows[i] * a.ldb + col;
-        if (wide) {
-          const f32x4 b0 = reinterpret_cast<const f32x4*>(base)[0];
-          const f32x4 b1 = reinterpret_cast<const f32x4*>(base)[1];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] += e < 4 ? b0[e & 3] : b1[e & 3];
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (e < valid) v[e] += base[e];
-        }
-      }
-      const int64_t at = (int64_t)rows[i] * a.ldo + col;
-      if constexpr (kOut16) {
-        uint16_t* out = static_cast<uint16_t*>(a.out) + at;
-        uint32_t b[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) b[e] = bf16_bits(v[e]);
-        if (wide) {
-          *reinterpret_cast<uint4*>(out) = make_uint4(b[0] | b[1] << 16, b[2] | b[3] << 16,
-                                                      b[4] | b[5] << 16, b[6] | b[7] << 16);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (e < valid) out[e] = (uint16_t)b[e];
-        }
-      } else {
-        float* out = static_cast<float*>(a.out) + at;
-        if (wide) {
-          reinterpret_cast<f32x4*>(out)[0] = f32x4{v[0], v[1], v[2], v[3]};
-          reinterpret_cast<f32x4*>(out)[1] = f32x4{v[4], v[5], v[6], v[7]};
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (e < valid) out[e] = v[e];
+            if ((e & 1 ? u[e >> 1] >> 16 : u[e >> 1] & 0xFFFFu) < a.drop.threshold)
+              acc[i][e >> 2][e & 3] = 0.0f;
         }
       }
     }
+    const auto store = [&](bool check) {
+      const int col = c0 + lane_col;
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        f32x4* mine = turn[wave];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < 2; ++j) mine[r16 * 8 + ((2 * g + j) ^ (r16 & 7))] = acc[i][j];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int h = 0; h < kLoads / kRows; ++h) {
+          const int q = h * (64 / kLanes) + sub, row = order[i * 16 + q];
+          const int64_t at = (int64_t)((uint64_t)(uint32_t)row * (uint32_t)a.ldo) + col;
+          if constexpr (kAligned) {
+            const f32x4 v = mine[q * 8 + ((lane & 7) ^ (q & 7))] + held[i][h];
+            if (check && (row < 0 || col >= end)) continue;
+            if constexpr (kOut16)
+              *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at) =
+                  make_uint2(bf16_bits(v[0]) | bf16_bits(v[1]) << 16,
+                             bf16_bits(v[2]) | bf16_bits(v[3]) << 16);
+            else
+              *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = v;
+          } else {
+            const float v = reinterpret_cast<const float*>(
+                                mine)[(q * 8 + ((lane_col >> 2) ^ (q & 7))) * 4 + (lane_col & 3)] +
+                            held[i][h >> 2][h & 3];
+            if (check && (row < 0 || col >= end)) continue;
+            if constexpr (kOut16)
+              static_cast<uint16_t*>(a.out)[at] = (uint16_t)bf16_bits(v);
+            else
+              static_cast<float*>(a.out)[at] = v;
+          }
+        }
+      }
+    };
+    if (whole && block + 128 <= end)
+      store(false);
+    else
+      store(true);
+  }
+}
+
+template <int kT, bool kDx, bool kOut16, bool kAligned>
+void launch(const ExpandArgs& a, int64_t tiles, int width, hipStream_t stream) {
+  const dim3 grid = tile_grid((a.cols + width - 1) / width, tiles);
+  const int n = (int)tiles;
+  switch (padded_rank(a.rank)) {
+    case 16: expand_kernel<kT, 16, kDx, kOut16, kAligned><<<grid, kThreads, 0, stream>>>(a, width, n); break;
+    case 32: expand_kernel<kT, 32, kDx, kOut16, kAligned><<<grid, kThreads, 0, stream>>>(a, width, n); break;
+    case 64: expand_kernel<kT, 64, kDx, kOut16, kAligned><<<grid, kThreads, 0, stream>>>(a, width, n); break;
+    case 128: expand_kernel<kT, 128, kDx, kOut16, kAligned><<<grid, kThreads, 0, stream>>>(a, width, n); break;
+    default: expand_kernel<kT, 256, kDx, kOut16, kAligned><<<grid, kThreads, 0, stream>>>(a, width, n); break;
   }
 }
 
 template <int kT, bool kDx, bool kOut16>
 void launch(const ExpandArgs& a, int64_t tiles, int width, bool aligned, hipStream_t stream) {
-  const dim3 grid((unsigned)tiles, (unsigned)((a.cols + width - 1) / width));
-  switch (padded_rank(a.rank)) {
-    case 16: expand_kernel<kT, 16, kDx, kOut16><<<grid, kThreads, 0, stream>>>(a, width, aligned); break;
-    case 32: expand_kernel<kT, 32, kDx, kOut16><<<grid, kThreads, 0, stream>>>(a, width, aligned); break;
-    case 64: expand_kernel<kT, 64, kDx, kOut16><<<grid, kThreads, 0, stream>>>(a, width, aligned); break;
-    case 128: expand_kernel<kT, 128, kDx, kOut16><<<grid, kThreads, 0, stream>>>(a, width, aligned); break;
-    default: expand_kernel<kT, 256, kDx, kOut16><<<grid, kThreads, 0, stream>>>(a, width, aligned); break;
-  }
+  aligned ? launch<kT, kDx, kOut16, true>(a, tiles, width, stream)
+          : launch<kT, kDx, kOut16, false>(a, tiles, width, stream);
 }
 
 }  // namespace
@@ -177,10 +280,12 @@ hipError_t launch_adapter_expand(const ExpandArgs& a, int tile_rows, int64_t til
                                  bool out16, hipStream_t stream) {
   // columns per workgroup: wide enough that the terms are read seldom, as
   // long as the device stays full
-  int64_t width = (a.cols * tiles / 1024 + 127) / 128 * 128;
+  const int padded = padded_rank(a.rank);
+  int64_t width = a.cols * tiles / 1024;
+  if (width > 5 * padded) width = 5 * padded;
+  width = (width + 127) / 128 * 128;
   if (width < 128) width = 128;
-  if (width > 1024) width = 1024;
-  const bool aligned = ((uintptr_t)a.out & 15) == 0 && a.ldo % (out16 ? 8 : 4) == 0 &&
+  const bool aligned = a.cols % 4 == 0 && ((uintptr_t)a.out & (out16 ? 7 : 15)) == 0 && a.ldo % 4 == 0 &&
                        (!a.base || (((uintptr_t)a.base & 15) == 0 && a.ldb % 4 == 0));
   const bool small = tile_rows == 16;
   const int wd = (int)width;

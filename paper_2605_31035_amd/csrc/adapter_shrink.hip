@@ -16,7 +16,7 @@ constexpr int kThreads = 256;
 // group of dropout's draws.  With tiles of 64 rows each wave takes 16 of
 // them, with tiles of 16 a quarter of every chunk, joined at the end.
 template <int kT, int kRank, bool kTransposed>
-__global__ __launch_bounds__(kThreads) void shrink_kernel(ShrinkArgs a) {
+__global__ __launch_bounds__(kThreads) void shrink_kernel(ShrinkArgs a, int tiles) {
   constexpr int kC = kT == 16 || kRank <= 64 ? 128 : 64;
   constexpr int kSlots = kC / 8;
   constexpr int kTiles = kRank / 16;
@@ -27,8 +27,10 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(ShrinkArgs a) {
   constexpr int kLds = kRank * kSlots > (kT == 16 ? 4 * kTiles * 64 : 0) ? kRank * kSlots
                                                                         : 4 * kTiles * 64;
   __shared__ uint4 lds[kLds];
-  const int tile = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int tile = blockIdx.z * gridDim.y + blockIdx.y, piece = blockIdx.x;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int r16 = lane & 15, g = lane >> 4;
+  if (tile >= tiles) return;
   const int l = a.plan.tile_adapter[tile];
   if (l < 0 || l >= a.adapters) return;
   const int rank = rank_of(a.ranks, l, a.rank);
@@ -39,8 +41,8 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(ShrinkArgs a) {
   const int64_t draw = (int64_t)row * (a.depth / 8);       // dropout: depth % 8 == 0
 
   const int chunks = (a.depth + kC - 1) / kC;
-  const int c0 = (int)((int64_t)chunks * blockIdx.y / a.splits);
-  const int c1 = (int)((int64_t)chunks * (blockIdx.y + 1) / a.splits);
+  const int c0 = (int)((int64_t)chunks * piece / a.splits);
+  const int c1 = (int)((int64_t)chunks * (piece + 1) / a.splits);
 
   uint4 xr[kSteps];
   uint4 wr[kPer][kTransposed ? 8 : 1];
@@ -74,8 +76,12 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(ShrinkArgs a) {
   f32x4 acc[kTiles];
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  if (c0 < c1) load(c0);
-  for (int chunk = c0; chunk < c1; ++chunk) {
+  // each tile begins elsewhere in the piece (see tile_grid on memory channels)
+  const int count = c1 - c0;
+  int chunk = c0 + (count > 0 ? tile % count : 0);
+  if (count > 0) load(chunk);
+  for (int done = 0; done < count; ++done) {
+    const int next = chunk + 1 < c1 ? chunk + 1 : c0;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -100,7 +106,7 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(ShrinkArgs a) {
                                        a.drop.threshold));
     }
     __syncthreads();
-    if (chunk + 1 < c1) load(chunk + 1);
+    if (done + 1 < count) load(next);
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
       const int slot = (kT == 16 ? wave * 4 : s * 4) + g;
@@ -108,9 +114,10 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(ShrinkArgs a) {
       for (int i = 0; i < kTiles; ++i)
         acc[i] = mfma16(lds[lds_slot<kSlots>(i * 16 + r16, slot)], xf[s], acc[i]);
     }
+    chunk = next;
   }
 
-  float* part = a.part + (int64_t)blockIdx.y * a.positions * a.rank;
+  float* part = a.part + (int64_t)piece * a.positions * a.rank;
   if constexpr (kT == 16) {
     __syncthreads();
     f32x4* sums = reinterpret_cast<f32x4*>(lds);
@@ -135,13 +142,14 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(ShrinkArgs a) {
 
 template <int kT, bool kTransposed>
 void launch(const ShrinkArgs& a, int64_t tiles, hipStream_t stream) {
-  const dim3 grid((unsigned)tiles, (unsigned)a.splits);
+  const dim3 grid = tile_grid(a.splits, tiles);
+  const int count = (int)tiles;
   switch (padded_rank(a.rank)) {
-    case 16: shrink_kernel<kT, 16, kTransposed><<<grid, kThreads, 0, stream>>>(a); break;
-    case 32: shrink_kernel<kT, 32, kTransposed><<<grid, kThreads, 0, stream>>>(a); break;
-    case 64: shrink_kernel<kT, 64, kTransposed><<<grid, kThreads, 0, stream>>>(a); break;
-    case 128: shrink_kernel<kT, 128, kTransposed><<<grid, kThreads, 0, stream>>>(a); break;
-    default: shrink_kernel<kT, 256, kTransposed><<<grid, kThreads, 0, stream>>>(a); break;
+    case 16: shrink_kernel<kT, 16, kTransposed><<<grid, kThreads, 0, stream>>>(a, count); break;
+    case 32: shrink_kernel<kT, 32, kTransposed><<<grid, kThreads, 0, stream>>>(a, count); break;
+    case 64: shrink_kernel<kT, 64, kTransposed><<<grid, kThreads, 0, stream>>>(a, count); break;
+    case 128: shrink_kernel<kT, 128, kTransposed><<<grid, kThreads, 0, stream>>>(a, count); break;
+    default: shrink_kernel<kT, 256, kTransposed><<<grid, kThreads, 0, stream>>>(a, count); break;
   }
 }
 

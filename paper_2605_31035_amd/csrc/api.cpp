@@ -521,6 +521,9 @@ bool valid_adapters(int64_t m, int64_t n, int64_t k, int64_t rank, int64_t adapt
          k % 8 == 0 && rank >= 8 && rank <= mixfp4::kMaxRank && rank % 8 == 0;
 }
 
+// Row pitches that a kernel multiplies in 32 bits.
+bool valid_pitch(int64_t ld, int64_t cols) { return ld >= cols && ld < (int64_t(1) << 32); }
+
 bool valid_type(int32_t t) { return t == MIXFP4_TYPE_F32 || t == MIXFP4_TYPE_BF16; }
 uintptr_t type_bytes(int32_t t) { return t == MIXFP4_TYPE_BF16 ? 2 : 4; }
 
@@ -587,7 +590,8 @@ int mixfp4_adapter(const uint16_t* x, int64_t ldx, const uint16_t* a, const uint
   if (!valid_adapters(m, n, k, rank, adapters) || !drop_params(p, seed, offset, &q.drop))
     return MIXFP4_ERR_SHAPE;
   if (m == 0) return MIXFP4_OK;
-  if (ldx < k || ldx % 8 != 0 || (c && ldc < n) || ldo < n) return MIXFP4_ERR_SHAPE;
+  if (!valid_pitch(ldx, k) || ldx % 8 != 0 || (c && !valid_pitch(ldc, n)) || !valid_pitch(ldo, n))
+    return MIXFP4_ERR_SHAPE;
   if (!x || !a || !b || !plan || !out || !workspace) return MIXFP4_ERR_NULL;
   if (workspace_bytes < mixfp4::adapter_workspace(m, n, k, rank, adapters, false))
     return MIXFP4_ERR_SHAPE;
@@ -614,8 +618,8 @@ int mixfp4_adapter_backward(const uint16_t* dy, int64_t lddy, const uint16_t* x,
   mixfp4::AdapterArgs q{};
   if (!valid_adapters(m, n, k, rank, adapters) || !drop_params(p, seed, offset, &q.drop))
     return MIXFP4_ERR_SHAPE;
-  if (m > 0 && (ldx < k || ldx % 8 != 0 || lddy < n || lddy % 8 != 0 || (dx_in && lddx_in < k) ||
-                lddx < k))
+  if (m > 0 && (!valid_pitch(ldx, k) || ldx % 8 != 0 || !valid_pitch(lddy, n) || lddy % 8 != 0 ||
+                (dx_in && !valid_pitch(lddx_in, k)) || !valid_pitch(lddx, k)))
     return MIXFP4_ERR_SHAPE;
   if (!plan || !da || !db || !workspace) return MIXFP4_ERR_NULL;
   if (m > 0 && (!dy || !x || !t || !a || !b || !dx)) return MIXFP4_ERR_NULL;
