@@ -281,7 +281,7 @@ hipError_t launch_adapter_expand(const ExpandArgs& a, int tile_rows, int64_t til
   // columns per workgroup: wide enough that the terms are read seldom, as
   // long as the device stays full
   const int padded = padded_rank(a.rank);
-  int64_t width = a.cols * tiles / 1024;
+  int64_t width = a.cols * tiles / 3072;
   if (width > 5 * padded) width = 5 * padded;
   width = (width + 127) / 128 * 128;
   if (width < 128) width = 128;

@@ -1,6 +1,8 @@
 // The gradients of the adapters: dA_l = sum u_i^T (keep_i x_i) and
 // dB_l = sum dy_i^T t_i over the rows i of adapter l, products whose
 // contraction runs along the rows.
+#include <type_traits>
+
 #include "adapter.h"
 
 namespace mixfp4 {
@@ -9,8 +11,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kCols = 128;     // columns of x or dy of a workgroup
-constexpr int kDepth = 128;    // positions of a step
-constexpr int kSlots = kDepth / 8;
 
 // Positions of the pieces: whole tiles, split evenly over those in use.
 __device__ __forceinline__ int64_t piece_begin(int64_t tiles, int s, int splits) {
@@ -18,41 +18,51 @@ __device__ __forceinline__ int64_t piece_begin(int64_t tiles, int s, int splits)
 }
 
 // One workgroup: 128 columns, all of the rank, one piece of the positions.
-// It walks the adapters that its piece holds.  Each step transposes 128
-// positions x 128 columns through registers into LDS (8 x 8 per thread: eight
-// 16-byte loads of eight rows, on which dropout's draws are made, one group
-// each), so that an operand's 8 consecutive positions are one LDS read; the
-// terms come transposed from the join.  An adapter within one piece is
-// written at once, one across pieces as partial sums (at most two per piece:
-// the one that enters it and the one that leaves it) for sum_kernel.
+// It walks the adapters that its piece holds, kDepth positions at a time.
+// The columns of x or dy are transposed through registers into LDS (8 rows by
+// 8 or 4 columns per thread; dropout's draws are made on the rows), the terms
+// come transposed from the join, so that an operand's 8 consecutive positions
+// are one LDS read.  The next step's reads are under way while a step is
+// multiplied.  An adapter within one piece is written at once, one across
+// pieces as partial sums (at most two per piece: the one that enters it and
+// the one that leaves it) for sum_kernel.  A rank above 128 takes two
+// workgroups (r0), so that the sums stay in registers.
 template <int kRank, bool kDb>
-__global__ __launch_bounds__(kThreads) void grad_kernel(GradArgs a) {
+__device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, int block, int piece,
+                                          int r0, uint4* lds) {
   constexpr int kTiles = kRank / 16;
-  __shared__ uint4 xt[kCols * kSlots];
+  constexpr int kDepth = kRank <= 64 ? 128 : 64;
+  constexpr int kSlots = kDepth / 8;
+  constexpr int kWidth = kDepth == 128 ? 8 : 4;            // columns of a thread's piece
+  constexpr int kGroups = kCols / kWidth;
+  constexpr int kTerms = 3 * kRank * kSlots;
+  constexpr int kPer = (kTerms + kThreads - 1) / kThreads;
+  using Row = std::conditional_t<kWidth == 8, uint4, uint2>;
+  uint4* xt = lds;
+  uint4* ut = lds + kCols * kSlots;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int r16 = lane & 15, g = lane >> 4;
-  const int col0 = blockIdx.x * kCols;
-  const int piece = blockIdx.y;
-  const int64_t tiles = a.plan.seg[a.adapters];
-  const int64_t t0 = piece_begin(tiles, piece, a.splits), t1 = piece_begin(tiles, piece + 1, a.splits);
-  const int64_t matrix = (int64_t)a.rank * a.cols;
-  const int cg = tid % 16, pg = tid / 16;
-  const int col = col0 + cg * 8;
+  const int col0 = block * kCols;
+  const int64_t tiles = q.plan.seg[q.adapters];
+  const int64_t t0 = piece_begin(tiles, piece, q.splits), t1 = piece_begin(tiles, piece + 1, q.splits);
+  const int64_t matrix = (int64_t)q.rank * a.cols;
+  const int cg = tid % kGroups, pg = tid / kGroups;
+  const int col = col0 + cg * kWidth;
 
   f32x4 acc[kTiles][2];
   const auto store = [&](float* to) {
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
       if constexpr (kDb) {
-        const int r = 16 * i + 4 * g;
+        const int r = r0 + 16 * i + 4 * g;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int n = col0 + wave * 32 + 16 * j + r16;
-          if (n < a.cols && r < a.rank) *reinterpret_cast<f32x4*>(to + (int64_t)n * a.rank + r) = acc[i][j];
+          if (n < a.cols && r < q.rank) *reinterpret_cast<f32x4*>(to + (int64_t)n * q.rank + r) = acc[i][j];
         }
       } else {
-        const int r = 16 * i + r16, c = col0 + wave * 32 + 8 * g;
-        if (r < a.rank && c < a.cols)
+        const int r = r0 + 16 * i + r16, c = col0 + wave * 32 + 8 * g;
+        if (r < q.rank && c < a.cols)
 #pragma unroll
           for (int j = 0; j < 2; ++j)
             *reinterpret_cast<f32x4*>(to + (int64_t)r * a.cols + c + 4 * j) = acc[i][j];
@@ -65,42 +75,107 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(GradArgs a) {
   };
 
   if (piece == 0)                  // adapters without rows
-    for (int l = 0; l < a.adapters; ++l)
-      if (a.plan.seg[l] == a.plan.seg[l + 1]) {
+    for (int l = 0; l < q.adapters; ++l)
+      if (q.plan.seg[l] == q.plan.seg[l + 1]) {
         clear();
         store(a.out + l * matrix);
       }
   if (t0 >= t1) return;
-  for (int l = a.plan.tile_adapter[t0]; l < a.adapters && a.plan.seg[l] < t1; ++l) {
-    const int64_t first = a.plan.seg[l], last = a.plan.seg[l + 1];
+
+  int rows[8], at_rows[8];         // of the next step's reads, of the reads under way
+  Row x[8];
+  uint4 u[kPer];
+  const auto load_rows = [&](int64_t p, int64_t p1) {
+    const int64_t at = p + pg * 8;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) rows[j] = -1;
+    if (at < p1) {
+      const int4 lo = *reinterpret_cast<const int4*>(q.plan.order + at);
+      const int4 hi = *reinterpret_cast<const int4*>(q.plan.order + at + 4);
+      rows[0] = lo.x, rows[1] = lo.y, rows[2] = lo.z, rows[3] = lo.w;
+      rows[4] = hi.x, rows[5] = hi.y, rows[6] = hi.z, rows[7] = hi.w;
+    }
+  };
+  const bool inside = col + kWidth <= a.cols;
+  const auto load = [&](int64_t p, int64_t p1) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) at_rows[j] = rows[j];
+    if (inside) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t row = rows[j] < 0 ? 0u : (uint32_t)rows[j];
+        x[j] = *reinterpret_cast<const Row*>(a.src + (uint64_t)row * (uint32_t)a.ld + col);
+      }
+    } else {
+      // the last columns, by element: nothing behind them is read
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t row = rows[j] < 0 ? 0u : (uint32_t)rows[j];
+        const uint4 v = load8(a.src + (uint64_t)row * (uint32_t)a.ld, col, a.cols);
+        if constexpr (kWidth == 8) x[j] = v; else x[j] = make_uint2(v.x, v.y);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int e = tid + i * kThreads;
+      const int64_t pos = p + e % kSlots * 8;
+      const int h = e / (kRank * kSlots), r = e / kSlots - h * kRank;
+      const uint16_t* from =
+          a.terms_t + (int64_t)(h * q.padded + r0 + r) * q.positions + (pos < p1 ? pos : p);
+      if (kTerms % kThreads == 0 || e < kTerms) u[i] = *reinterpret_cast<const uint4*>(from);
+    }
+  };
+
+  for (int l = q.plan.tile_adapter[t0]; l < q.adapters && q.plan.seg[l] < t1; ++l) {
+    const int64_t first = q.plan.seg[l], last = q.plan.seg[l + 1];
     if (first == last) continue;
-    const int64_t p0 = (first > t0 ? first : t0) * a.tile_rows;
-    const int64_t p1 = (last < t1 ? last : t1) * a.tile_rows;
+    const int64_t p0 = (first > t0 ? first : t0) * q.tile_rows;
+    const int64_t p1 = (last < t1 ? last : t1) * q.tile_rows;
     clear();
+    load_rows(p0, p1);
+    load(p0, p1);
+    load_rows(p0 + kDepth, p1);
     for (int64_t p = p0; p < p1; p += kDepth) {
-      uint4 v[8], q[8];
-      const int64_t at = p + pg * 8;
-      int row[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) row[j] = at < p1 ? a.plan.order[at + j] : -1;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        v[j] = row[j] >= 0 ? load8(a.src + (int64_t)row[j] * a.ld, col, a.cols)
-                           : make_uint4(0, 0, 0, 0);
-      if (!kDb && a.drop.threshold)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (row[j] >= 0 && col < a.cols)
-            v[j] = and4(v[j], keep_masks(block_draws((int64_t)row[j] * (a.cols / 8) + col / 8,
-                                                     a.drop.key), a.drop.threshold));
-      transpose8(v, q);
+      for (int j = 0; j < 8; ++j) {
+        if (at_rows[j] < 0) {
+          x[j] = Row{};
+        } else if (!kDb && q.drop.threshold) {
+          const uint4 m = keep_masks(block_draws((int64_t)at_rows[j] * (a.cols / 8) + col / 8, q.drop.key),
+                                     q.drop.threshold);
+          if constexpr (kWidth == 8) {
+            x[j] = and4(x[j], m);
+          } else {
+            x[j].x &= col & 4 ? m.z : m.x;
+            x[j].y &= col & 4 ? m.w : m.y;
+          }
+        }
+      }
       __syncthreads();
+      if constexpr (kWidth == 8) {
+        uint4 v[8];
+        transpose8(x, v);
 #pragma unroll
-      for (int c = 0; c < 8; ++c) xt[lds_slot<kSlots>(cg * 8 + c, pg)] = q[c];
+        for (int c = 0; c < 8; ++c) xt[lds_slot<kSlots>(cg * 8 + c, pg)] = v[c];
+      } else {
+        uint4 v[4];
+        transpose8x4(x, v);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) xt[lds_slot<kSlots>(cg * 4 + c, pg)] = v[c];
+      }
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int e = tid + i * kThreads;
+        if (p + e % kSlots * 8 >= p1) u[i] = make_uint4(0, 0, 0, 0);
+        if (kTerms % kThreads == 0 || e < kTerms) ut[lds_slot<kSlots>(e / kSlots, e % kSlots)] = u[i];
+      }
       __syncthreads();
+      if (p + kDepth < p1) {
+        load(p + kDepth, p1);
+        load_rows(p + 2 * kDepth, p1);
+      }
 #pragma unroll
       for (int s = 0; s < kDepth / 32; ++s) {
-        const int64_t pos = p + 32 * s + 8 * g;
         if (p + 32 * s >= p1) break;
         uint4 xf[2];
 #pragma unroll
@@ -109,17 +184,14 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(GradArgs a) {
           xf[j] = xt[lds_slot<kSlots>(wave * 32 + c, 4 * s + g)];
         }
 #pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-          const uint16_t* t = a.terms_t + (int64_t)(16 * i + r16) * a.positions + pos;
+        for (int i = 0; i < kTiles; ++i)
 #pragma unroll
           for (int h = 2; h >= 0; --h) {             // the smallest term first
-            const uint4 u = pos < p1 ? *reinterpret_cast<const uint4*>(t + (int64_t)h * kRank * a.positions)
-                                     : make_uint4(0, 0, 0, 0);
+            const uint4 uf = ut[lds_slot<kSlots>(h * kRank + 16 * i + r16, 4 * s + g)];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-              acc[i][j] = kDb ? mfma16(u, xf[j], acc[i][j]) : mfma16(xf[j], u, acc[i][j]);
+              acc[i][j] = kDb ? mfma16(uf, xf[j], acc[i][j]) : mfma16(xf[j], uf, acc[i][j]);
           }
-        }
       }
     }
     if (first >= t0 && last <= t1)
@@ -129,63 +201,85 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(GradArgs a) {
   }
 }
 
+template <int kRank>
+__global__ __launch_bounds__(kThreads, 2) void grad_kernel(GradArgs q) {
+  constexpr int kSlots = kRank <= 64 ? 16 : 8;
+  __shared__ uint4 lds[(kCols + 3 * kRank) * kSlots];
+  // the workgroups of a piece side by side: they read the same rows
+  const int blocks_a = (q.a.cols + kCols - 1) / kCols, blocks = blocks_a + (q.b.cols + kCols - 1) / kCols;
+  const int piece = blockIdx.x / blocks, block = blockIdx.x % blocks;
+  if (block < blocks_a)
+    grad_body<kRank, false>(q.a, q, block, piece, blockIdx.y * kRank, lds);
+  else
+    grad_body<kRank, true>(q.b, q, block - blocks_a, piece, blockIdx.y * kRank, lds);
+}
+
 // The adapters across pieces: their partial sums, in the order of the pieces.
-__global__ __launch_bounds__(kThreads) void sum_kernel(GradArgs a) {
+__global__ __launch_bounds__(kThreads) void sum_kernel(GradArgs q) {
+  const GradSide& a = blockIdx.z ? q.b : q.a;
   const int l = blockIdx.y;
-  const int64_t tiles = a.plan.seg[a.adapters];
-  const int64_t first = a.plan.seg[l], last = a.plan.seg[l + 1];
+  const int64_t tiles = q.plan.seg[q.adapters];
+  const int64_t first = q.plan.seg[l], last = q.plan.seg[l + 1];
   if (first == last) return;
   int s0 = 0, s1 = 0;
-  for (int s = 1; s < a.splits; ++s) {
-    const int64_t b = piece_begin(tiles, s, a.splits);
+  for (int s = 1; s < q.splits; ++s) {
+    const int64_t b = piece_begin(tiles, s, q.splits);
     if (b <= first) s0 = s;
     if (b < last) s1 = s;
   }
   if (s0 == s1) return;
-  const int64_t matrix = (int64_t)a.rank * a.cols;
+  const int64_t matrix = (int64_t)q.rank * a.cols;
   for (int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4; i < matrix;
        i += (int64_t)gridDim.x * kThreads * 4) {
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
     for (int s = s0; s <= s1; ++s) {
-      if (piece_begin(tiles, s, a.splits) == piece_begin(tiles, s + 1, a.splits)) continue;
-      const int slot = 2 * s + (first >= piece_begin(tiles, s, a.splits));
+      if (piece_begin(tiles, s, q.splits) == piece_begin(tiles, s + 1, q.splits)) continue;
+      const int slot = 2 * s + (first >= piece_begin(tiles, s, q.splits));
       v += *reinterpret_cast<const f32x4*>(a.part + slot * matrix + i);
     }
     *reinterpret_cast<f32x4*>(a.out + l * matrix + i) = v;
   }
 }
 
-template <bool kDb>
-void launch(const GradArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)((a.cols + kCols - 1) / kCols), (unsigned)a.splits);
-  switch (padded_rank(a.rank)) {
-    case 16: grad_kernel<16, kDb><<<grid, kThreads, 0, stream>>>(a); break;
-    case 32: grad_kernel<32, kDb><<<grid, kThreads, 0, stream>>>(a); break;
-    case 64: grad_kernel<64, kDb><<<grid, kThreads, 0, stream>>>(a); break;
-    case 128: grad_kernel<128, kDb><<<grid, kThreads, 0, stream>>>(a); break;
-    default: grad_kernel<256, kDb><<<grid, kThreads, 0, stream>>>(a); break;
-  }
-}
+int64_t blocks_of(int64_t cols) { return (cols + kCols - 1) / kCols; }
 
 }  // namespace
 
-// Pieces of the positions: enough workgroups to fill the device, as long as
-// the partial sums (8 bytes an element, written and read) stay below a
-// quarter of src's bytes.
-int adapter_grad_splits(int64_t m, int64_t cols, int64_t rank) {
-  const int64_t blocks = (cols + kCols - 1) / kCols;
-  int64_t s = (512 + blocks - 1) / blocks;
-  if (s > m / (16 * rank)) s = m / (16 * rank);
-  return s < 1 ? 1 : (int)s;
+// Pieces of the positions.  More of them fill the device, in whole rounds of
+// two workgroups per compute unit at best, and write and read more partial
+// sums: 8 bytes an element of the gradients against 2 an element of x and dy.
+int adapter_grad_splits(int64_t m, int64_t n, int64_t k, int64_t rank) {
+  const int64_t blocks = (blocks_of(n) + blocks_of(k)) * (rank > 128 ? 2 : 1), round = 2 * compute_units();
+  int best = 1;
+  double score = 0.0;
+  for (int64_t s = 1; s <= 64 && (s == 1 || s * 256 <= m); ++s) {
+    const int64_t groups = blocks * s;
+    const double full = (double)groups / (double)((groups + round - 1) / round * round);
+    const double v = full / (1.0 + (s > 1 ? (double)(s * rank * 4) / (double)m : 0.0));
+    if (v > 1.02 * score) {
+      score = v;
+      best = (int)s;
+    }
+  }
+  return best;
 }
 
-hipError_t launch_adapter_grad(const GradArgs& a, bool db, hipStream_t stream) {
-  db ? launch<true>(a, stream) : launch<false>(a, stream);
+hipError_t launch_adapter_grad(const GradArgs& q, hipStream_t stream) {
+  const unsigned grid = (unsigned)((blocks_of(q.a.cols) + blocks_of(q.b.cols)) * q.splits);
+  switch (padded_rank(q.rank)) {
+    case 16: grad_kernel<16><<<grid, kThreads, 0, stream>>>(q); break;
+    case 32: grad_kernel<32><<<grid, kThreads, 0, stream>>>(q); break;
+    case 64: grad_kernel<64><<<grid, kThreads, 0, stream>>>(q); break;
+    case 128: grad_kernel<128><<<grid, kThreads, 0, stream>>>(q); break;
+    default: grad_kernel<128><<<dim3(grid, 2), kThreads, 0, stream>>>(q); break;
+  }
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.splits == 1) return e;
-  const int64_t blocks = ((int64_t)a.rank * a.cols + 4 * kThreads - 1) / (4 * kThreads);
-  sum_kernel<<<dim3((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)a.adapters), kThreads, 0,
-               stream>>>(a);
+  if (e != hipSuccess || q.splits == 1) return e;
+  const int64_t cols = q.a.cols > q.b.cols ? q.a.cols : q.b.cols;
+  const int64_t blocks = ((int64_t)q.rank * cols + 4 * kThreads - 1) / (4 * kThreads);
+  sum_kernel<<<dim3((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)q.adapters, 2), kThreads, 0,
+               stream>>>(q);
   return hipGetLastError();
 }
 

@@ -22,7 +22,7 @@ struct Pass {
   int tile_rows;
   int64_t tiles, positions;
   int padded, width;                       // terms: padded rank, at least 32 of them
-  int splits, splits_a, splits_b;
+  int splits, grad_splits;
   float *part, *part_a, *part_b;
   uint16_t *terms, *terms_t, *t_t;
   int64_t bytes;
@@ -34,8 +34,7 @@ struct Pass {
     padded = padded_rank(rank);
     width = padded < 32 ? 32 : padded;
     splits = adapter_shrink_splits(tiles, backward ? n : k, rank);
-    splits_a = adapter_grad_splits(m, k, rank);
-    splits_b = adapter_grad_splits(m, n, rank);
+    grad_splits = backward ? adapter_grad_splits(m, n, k, rank) : 1;
     Carver c{static_cast<uint8_t*>(ws)};
     part = c.take<float>(4 * splits * positions * rank);
     terms = c.take<uint16_t>(4 * positions * width);
@@ -44,8 +43,10 @@ struct Pass {
     if (backward) {
       terms_t = c.take<uint16_t>(6 * positions * padded);
       t_t = c.take<uint16_t>(6 * positions * padded);
-      if (splits_a > 1) part_a = c.take<float>(8 * splits_a * rank * k);
-      if (splits_b > 1) part_b = c.take<float>(8 * splits_b * rank * n);
+      if (grad_splits > 1) {
+        part_a = c.take<float>(8 * grad_splits * rank * k);
+        part_b = c.take<float>(8 * grad_splits * rank * n);
+      }
     }
     bytes = c.used;
   }
@@ -79,14 +80,10 @@ hipError_t launch_adapter(const AdapterArgs& a, hipStream_t stream) {
 hipError_t launch_adapter_backward(const AdapterArgs& a, hipStream_t stream) {
   const Pass p(a.m, a.n, a.k, a.rank, a.adapters, true, a.workspace);
   const int rank = (int)a.rank, adapters = (int)a.adapters;
-  const GradArgs ga{a.x, a.ldx, p.terms_t, a.plan, a.drop, p.positions, (int)a.k, rank, adapters,
-                    p.splits_a, p.tile_rows, p.part_a, a.da};
-  const GradArgs gb{a.dy, a.lddy, p.t_t, a.plan, {}, p.positions, (int)a.n, rank, adapters,
-                    p.splits_b, p.tile_rows, p.part_b, a.db};
-  if (a.m == 0) {                          // gradients of zero
-    const hipError_t e = launch_adapter_grad(ga, false, stream);
-    return e != hipSuccess ? e : launch_adapter_grad(gb, true, stream);
-  }
+  const GradArgs grad{{a.x, a.ldx, p.terms_t, p.part_a, a.da, (int)a.k},
+                      {a.dy, a.lddy, p.t_t, p.part_b, a.db, (int)a.n},
+                      a.plan, a.drop, p.positions, rank, p.padded, adapters, p.grad_splits, p.tile_rows};
+  if (a.m == 0) return launch_adapter_grad(grad, stream);      // gradients of zero
   hipError_t e = launch_adapter_shrink(
       {a.dy, a.lddy, a.b, a.ranks, a.plan, {}, (int)a.n, rank, adapters, p.splits, p.positions, p.part},
       p.tile_rows, p.tiles, true, stream);
@@ -101,9 +98,7 @@ hipError_t launch_adapter_backward(const AdapterArgs& a, hipStream_t stream) {
                              (int)a.k, rank, adapters},
                             p.tile_rows, p.tiles, true, false, stream);
   if (e != hipSuccess) return e;
-  e = launch_adapter_grad(ga, false, stream);
-  if (e != hipSuccess) return e;
-  return launch_adapter_grad(gb, true, stream);
+  return launch_adapter_grad(grad, stream);
 }
 
 }  // namespace mixfp4

@@ -360,21 +360,25 @@ struct ExpandArgs {
 };
 hipError_t launch_adapter_expand(const ExpandArgs& a, int tile_rows, int64_t tiles, bool dx,
                                  bool out16, hipStream_t stream);
-// dA_l [rank, cols] (src = x with dropout, terms of u) or dB_l [cols, rank]
-// (src = dy, terms of t), the positions in `splits` pieces whose partial sums
-// are joined.
-struct GradArgs {
+// dA_l [rank, k] (src = x with dropout, terms of u) and dB_l [n, rank] (src =
+// dy, terms of t), the positions in `splits` pieces whose partial sums are
+// joined.
+struct GradSide {
   const uint16_t* src;
   int64_t ld;
   const uint16_t* terms_t;
+  float* part;             // [2 splits][rank * cols], NULL for one piece
+  float* out;
+  int cols;
+};
+struct GradArgs {
+  GradSide a, b;
   AdapterPlan plan;
   DropParams drop;
   int64_t positions;
-  int cols, rank, adapters, splits, tile_rows;
-  float* part;             // [2 splits][rank * cols]
-  float* out;
+  int rank, padded, adapters, splits, tile_rows;
 };
-int adapter_grad_splits(int64_t m, int64_t cols, int64_t rank);
-hipError_t launch_adapter_grad(const GradArgs& a, bool db, hipStream_t stream);
+int adapter_grad_splits(int64_t m, int64_t n, int64_t k, int64_t rank);
+hipError_t launch_adapter_grad(const GradArgs& a, hipStream_t stream);
 
 }  // namespace mixfp4
