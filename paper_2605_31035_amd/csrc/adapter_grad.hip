@@ -10,14 +10,17 @@ namespace mixfp4 {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kCols = 128;     // columns of x or dy of a workgroup
+
+// Columns of x or dy of a workgroup: the more, the fewer reads of the terms;
+// the sums of 256 columns by a rank of 64 take 64 registers of each lane.
+constexpr int cols_of(int padded) { return padded <= 64 ? 256 : 128; }
 
 // Positions of the pieces: whole tiles, split evenly over those in use.
 __device__ __forceinline__ int64_t piece_begin(int64_t tiles, int s, int splits) {
   return tiles * s / splits;
 }
 
-// One workgroup: 128 columns, all of the rank, one piece of the positions.
+// One workgroup: 256 or 128 columns, all of the rank, one piece of the positions.
 // It walks the adapters that its piece holds, kDepth positions at a time.
 // The columns of x or dy are transposed through registers into LDS (8 rows by
 // 8 or 4 columns per thread; dropout's draws are made on the rows), the terms
@@ -31,9 +34,10 @@ template <int kRank, bool kDb>
 __device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, int block, int piece,
                                           int r0, uint4* lds) {
   constexpr int kTiles = kRank / 16;
-  constexpr int kDepth = kRank <= 64 ? 128 : 64;
+  constexpr int kCols = cols_of(kRank), kSide = kCols / 64; // 16-column tiles of a wave
+  constexpr int kDepth = 64;
   constexpr int kSlots = kDepth / 8;
-  constexpr int kWidth = kDepth == 128 ? 8 : 4;            // columns of a thread's piece
+  constexpr int kWidth = kCols / 32;                       // columns of a thread's piece
   constexpr int kGroups = kCols / kWidth;
   constexpr int kTerms = 3 * kRank * kSlots;
   constexpr int kPer = (kTerms + kThreads - 1) / kThreads;
@@ -49,29 +53,34 @@ __device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, 
   const int cg = tid % kGroups, pg = tid / kGroups;
   const int col = col0 + cg * kWidth;
 
-  f32x4 acc[kTiles][2];
+  f32x4 acc[kTiles][kSide];
+  const int wave_col = wave * 16 * kSide;
   const auto store = [&](float* to) {
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
       if constexpr (kDb) {
         const int r = r0 + 16 * i + 4 * g;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int n = col0 + wave * 32 + 16 * j + r16;
+        for (int j = 0; j < kSide; ++j) {
+          const int n = col0 + wave_col + 16 * j + r16;
           if (n < a.cols && r < q.rank) *reinterpret_cast<f32x4*>(to + (int64_t)n * q.rank + r) = acc[i][j];
         }
       } else {
-        const int r = r0 + 16 * i + r16, c = col0 + wave * 32 + 8 * g;
-        if (r < q.rank && c < a.cols)
+        const int r = r0 + 16 * i + r16;
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-            *reinterpret_cast<f32x4*>(to + (int64_t)r * a.cols + c + 4 * j) = acc[i][j];
+        for (int j = 0; j < kSide; ++j) {
+          const int c = col0 + wave_col + 32 * (j >> 1) + 8 * g;
+          if (r < q.rank && c < a.cols)
+            *reinterpret_cast<f32x4*>(to + (int64_t)r * a.cols + c + 4 * (j & 1)) = acc[i][j];
+        }
       }
     }
   };
   const auto clear = [&]() {
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) acc[i][0] = acc[i][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int j = 0; j < kSide; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   };
 
   if (piece == 0)                  // adapters without rows
@@ -177,11 +186,11 @@ __device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, 
 #pragma unroll
       for (int s = 0; s < kDepth / 32; ++s) {
         if (p + 32 * s >= p1) break;
-        uint4 xf[2];
+        uint4 xf[kSide];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int c = kDb ? 16 * j + r16 : 8 * (r16 >> 2) + 4 * j + (r16 & 3);
-          xf[j] = xt[lds_slot<kSlots>(wave * 32 + c, 4 * s + g)];
+        for (int j = 0; j < kSide; ++j) {
+          const int c = kDb ? 16 * j + r16 : 32 * (j >> 1) + 8 * (r16 >> 2) + 4 * (j & 1) + (r16 & 3);
+          xf[j] = xt[lds_slot<kSlots>(wave_col + c, 4 * s + g)];
         }
 #pragma unroll
         for (int i = 0; i < kTiles; ++i)
@@ -189,7 +198,7 @@ __device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, 
           for (int h = 2; h >= 0; --h) {             // the smallest term first
             const uint4 uf = ut[lds_slot<kSlots>(h * kRank + 16 * i + r16, 4 * s + g)];
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < kSide; ++j)
               acc[i][j] = kDb ? mfma16(uf, xf[j], acc[i][j]) : mfma16(xf[j], uf, acc[i][j]);
           }
       }
@@ -203,8 +212,8 @@ __device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, 
 
 template <int kRank>
 __global__ __launch_bounds__(kThreads, 2) void grad_kernel(GradArgs q) {
-  constexpr int kSlots = kRank <= 64 ? 16 : 8;
-  __shared__ uint4 lds[(kCols + 3 * kRank) * kSlots];
+  constexpr int kCols = cols_of(kRank);
+  __shared__ uint4 lds[(kCols + 3 * kRank) * 8];
   // the workgroups of a piece side by side: they read the same rows
   const int blocks_a = (q.a.cols + kCols - 1) / kCols, blocks = blocks_a + (q.b.cols + kCols - 1) / kCols;
   const int piece = blockIdx.x / blocks, block = blockIdx.x % blocks;
@@ -242,7 +251,10 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(GradArgs q) {
   }
 }
 
-int64_t blocks_of(int64_t cols) { return (cols + kCols - 1) / kCols; }
+int64_t blocks_of(int64_t cols, int64_t rank) {
+  const int c = cols_of(padded_rank(rank));
+  return (cols + c - 1) / c;
+}
 
 }  // namespace
 
@@ -250,7 +262,7 @@ int64_t blocks_of(int64_t cols) { return (cols + kCols - 1) / kCols; }
 // two workgroups per compute unit at best, and write and read more partial
 // sums: 8 bytes an element of the gradients against 2 an element of x and dy.
 int adapter_grad_splits(int64_t m, int64_t n, int64_t k, int64_t rank) {
-  const int64_t blocks = (blocks_of(n) + blocks_of(k)) * (rank > 128 ? 2 : 1), round = 2 * compute_units();
+  const int64_t blocks = (blocks_of(n, rank) + blocks_of(k, rank)) * (rank > 128 ? 2 : 1), round = 2 * compute_units();
   int best = 1;
   double score = 0.0;
   for (int64_t s = 1; s <= 64 && (s == 1 || s * 256 <= m); ++s) {
@@ -266,7 +278,7 @@ int adapter_grad_splits(int64_t m, int64_t n, int64_t k, int64_t rank) {
 }
 
 hipError_t launch_adapter_grad(const GradArgs& q, hipStream_t stream) {
-  const unsigned grid = (unsigned)((blocks_of(q.a.cols) + blocks_of(q.b.cols)) * q.splits);
+  const unsigned grid = (unsigned)((blocks_of(q.a.cols, q.rank) + blocks_of(q.b.cols, q.rank)) * q.splits);
   switch (padded_rank(q.rank)) {
     case 16: grad_kernel<16><<<grid, kThreads, 0, stream>>>(q); break;
     case 32: grad_kernel<32><<<grid, kThreads, 0, stream>>>(q); break;
