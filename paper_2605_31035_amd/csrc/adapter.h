@@ -78,6 +78,11 @@ __device__ __forceinline__ uint4 load8(const uint16_t* row, int col, int cols) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// Waits for all of the wave's loads: at the end of a branch that loads, so
+// that the code behind it need not wait on its account (s_waitcnt vmcnt(0),
+// the other counters at their maximum).
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }
+
 // 8 bf16 with those from element `valid` on cleared.
 __device__ __forceinline__ uint4 clear_from(uint4 v, int valid) {
   if (valid >= 8) return v;

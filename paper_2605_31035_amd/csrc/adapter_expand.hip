@@ -1,6 +1,8 @@
 // The wide products of the adapters: out = c + terms B_l^T and
 // dx = dx0 + keep (terms A_l), where the terms are s_l t or s_l z u in two
 // bf16 parts (adapter.h).
+#include <type_traits>
+
 #include "adapter.h"
 
 namespace mixfp4 {
@@ -19,9 +21,10 @@ constexpr int kThreads = 256;
 // 4 bytes each).  What the next block needs from memory is requested before
 // this block is stored: loads behind stores wait for them.  Loads are made
 // without branches, from a row or column that is there in place of one that
-// is not; only tiles and blocks that are not full look at each store.
+// is not (behind the last block, from one address): with loads in a branch
+// each wait would have to assume that none are under way.  Only tiles and blocks that are not full look at each store.
 template <int kT, int kRank, bool kDx, bool kOut16, bool kAligned>
-__global__ __launch_bounds__(kThreads) void expand_kernel(ExpandArgs a, int width, int tiles) {
+__global__ __launch_bounds__(kThreads, kRank <= 128 ? 2 : 1) void expand_kernel(ExpandArgs a, int width, int tiles) {
   constexpr int kWide = kRank < 32 ? 32 : kRank;     // terms per part
   constexpr int kSteps = kWide / 32;
   constexpr int kRows = kT / 16;
@@ -62,8 +65,7 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(ExpandArgs a, int widt
   }
   uint4 wf[kDx ? 1 : kPieces];
   uint2 wp[kDx ? kPieces : 1][8];
-  const auto load_w = [&](int block) {
-    if (rank == 0) return;
+  const auto load_w = [&](int block, bool there) {
     if constexpr (kDx) {
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) {
@@ -73,7 +75,7 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(ExpandArgs a, int widt
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int r = rb * 8 + j < rank ? rb * 8 + j : 0;
-          wp[i][j] = *reinterpret_cast<const uint2*>(w + (int64_t)r * a.cols + col);
+          wp[i][j] = *reinterpret_cast<const uint2*>(w + (there ? (int64_t)r * a.cols + col : 0));
         }
       }
     } else {
@@ -82,12 +84,12 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(ExpandArgs a, int widt
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) {
         const int p = lane + 64 * i;
-        const bool there = (piece_col[i] & 0xFF) < 32 && c0 + (piece_col[i] & 0xFF) < end;
-        wf[i] = *reinterpret_cast<const uint4*>(w + (there ? (int64_t)c0 * a.rank + p * 8 : 0));
+        const bool is = there && (piece_col[i] & 0xFF) < 32 && c0 + (piece_col[i] & 0xFF) < end;
+        wf[i] = *reinterpret_cast<const uint4*>(w + (is ? (int64_t)c0 * a.rank + p * 8 : 0));
       }
     }
   };
-  load_w(begin);
+  load_w(begin, true);
 
   if (tid < kT) order[tid] = a.plan.order[p0 + tid];
   if (rank > 0) {
@@ -113,37 +115,34 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(ExpandArgs a, int widt
   const bool whole = order[kT - 1] >= 0;
   const auto row_of = [&](int i) { return order[i * (64 / kLanes) + sub]; };
   f32x4 base[kRows][2];
-#pragma unroll
-  for (int i = 0; i < kRows; ++i) base[i][0] = base[i][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const auto load_base = [&](int block) {
-    if (!a.base) return;
+  const float* base_at = a.base ? a.base : reinterpret_cast<const float*>(a.w);
+  const bool has_base = a.base != nullptr;
+  const auto load_base = [&](int block, bool there) {
+    there = there && has_base;
     int col = block + wave * 32 + lane_col;
     col = col < end ? col : end - (kAligned ? 4 : 1);
-    const float* from = a.base + col;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       int row = row_of(i);
       row = row < 0 ? order[0] : row;
-      const float* p = from + (uint64_t)(uint32_t)row * (uint32_t)a.ldb;
+      const float* p = base_at + (there ? (uint64_t)(uint32_t)row * (uint32_t)a.ldb + col : 0u);
       if constexpr (kAligned)
-        base[i >> 1][i & 1] = *reinterpret_cast<const f32x4*>(p);
+        base[i >> 1][i & 1] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
       else
         base[i >> 3][(i >> 2) & 1][i & 3] = *p;
     }
   };
-  load_base(begin);
+  load_base(begin, true);
 
-  for (int block = begin; block < end; block += 128) {
-    const int c0 = block + wave * 32;
-    const bool more = block + 128 < end;
-    f32x4 acc[kRows][2], held[kRows][2];
+  // all blocks; kCheck: rows or columns may be missing
+  const auto run = [&](auto check) {
+    constexpr bool kCheck = decltype(check)::value;
+    for (int block = begin; block < end; block += 128) {
+      const int c0 = block + wave * 32;
+      const bool more = block + 128 < end;
+      f32x4 acc[kRows][2];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      acc[i][0] = acc[i][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      held[i][0] = base[i][0];
-      held[i][1] = base[i][1];
-    }
-    if (rank > 0) {
+      for (int i = 0; i < kRows; ++i) acc[i][0] = acc[i][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       if constexpr (kDx) {
         if (block > begin) __syncthreads();
 #pragma unroll
@@ -174,7 +173,7 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(ExpandArgs a, int widt
         }
         __builtin_amdgcn_wave_barrier();
       }
-      if (kAhead && more) load_w(block + 128);
+      if (kAhead) load_w(block + 128, more);
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
         if (s * 32 >= rank) break;
@@ -193,30 +192,20 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(ExpandArgs a, int widt
           }
         }
       }
-    }
-    if (more) {
-      if (!kAhead) load_w(block + 128);
-      load_base(block + 128);
-    }
-    if constexpr (kDx) {
-      if (a.drop.threshold) {
-        const int col = c0 + 8 * g;
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-          const int row = order[i * 16 + r16];
-          const uint4 d = block_draws((int64_t)row * (a.cols / 8) + col / 8, a.drop.key);
-          const uint32_t u[4] = {d.x, d.y, d.z, d.w};
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if ((e & 1 ? u[e >> 1] >> 16 : u[e >> 1] & 0xFFFFu) < a.drop.threshold)
-              acc[i][e >> 2][e & 3] = 0.0f;
-        }
-      }
-    }
-    const auto store = [&](bool check) {
-      const int col = c0 + lane_col;
+      if (!kAhead) load_w(block + 128, more);
 #pragma unroll
       for (int i = 0; i < kRows; ++i) {
+        if constexpr (kDx) {
+          if (a.drop.threshold) {
+            const int row = order[i * 16 + r16], col = c0 + 8 * g;
+            const uint4 d = block_draws((int64_t)row * (a.cols / 8) + col / 8, a.drop.key);
+            const uint32_t u[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if ((e & 1 ? u[e >> 1] >> 16 : u[e >> 1] & 0xFFFFu) < a.drop.threshold)
+                acc[i][e >> 2][e & 3] = 0.0f;
+          }
+        }
         f32x4* mine = turn[wave];
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -224,35 +213,45 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(ExpandArgs a, int widt
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int h = 0; h < kLoads / kRows; ++h) {
-          const int q = h * (64 / kLanes) + sub, row = order[i * 16 + q];
-          const int64_t at = (int64_t)((uint64_t)(uint32_t)row * (uint32_t)a.ldo) + col;
-          if constexpr (kAligned) {
-            const f32x4 v = mine[q * 8 + ((lane & 7) ^ (q & 7))] + held[i][h];
-            if (check && (row < 0 || col >= end)) continue;
-            if constexpr (kOut16)
-              *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at) =
-                  make_uint2(bf16_bits(v[0]) | bf16_bits(v[1]) << 16,
-                             bf16_bits(v[2]) | bf16_bits(v[3]) << 16);
-            else
-              *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = v;
-          } else {
-            const float v = reinterpret_cast<const float*>(
-                                mine)[(q * 8 + ((lane_col >> 2) ^ (q & 7))) * 4 + (lane_col & 3)] +
-                            held[i][h >> 2][h & 3];
-            if (check && (row < 0 || col >= end)) continue;
-            if constexpr (kOut16)
-              static_cast<uint16_t*>(a.out)[at] = (uint16_t)bf16_bits(v);
-            else
-              static_cast<float*>(a.out)[at] = v;
-          }
+          const int q = h * (64 / kLanes) + sub;
+          if constexpr (kAligned)
+            acc[i][h] = mine[q * 8 + ((lane & 7) ^ (q & 7))];
+          else
+            acc[i][h >> 2][h & 3] = reinterpret_cast<const float*>(
+                mine)[(q * 8 + ((lane_col >> 2) ^ (q & 7))) * 4 + (lane_col & 3)];
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (has_base) acc[i][h] += base[i][h];
+      }
+      load_base(block + 128, more);
+      const int col = c0 + lane_col;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int row = row_of(i);
+        if (kCheck && (row < 0 || col >= end)) continue;
+        const int64_t at = (int64_t)((uint64_t)(uint32_t)row * (uint32_t)a.ldo) + col;
+        if constexpr (kAligned) {
+          const f32x4 v = acc[i >> 1][i & 1];
+          if constexpr (kOut16)
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at) = make_uint2(
+                bf16_bits(v[0]) | bf16_bits(v[1]) << 16, bf16_bits(v[2]) | bf16_bits(v[3]) << 16);
+          else
+            __builtin_nontemporal_store(v, reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at));
+        } else {
+          const float v = acc[i >> 3][(i >> 2) & 1][i & 3];
+          if constexpr (kOut16)
+            static_cast<uint16_t*>(a.out)[at] = (uint16_t)bf16_bits(v);
+          else
+            static_cast<float*>(a.out)[at] = v;
         }
       }
-    };
-    if (whole && block + 128 <= end)
-      store(false);
-    else
-      store(true);
-  }
+    }
+  };
+  if (whole && (end - begin) % 128 == 0)
+    run(std::false_type{});
+  else
+    run(std::true_type{});
 }
 
 template <int kT, bool kDx, bool kOut16, bool kAligned>

@@ -109,20 +109,11 @@ __device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, 
   const auto load = [&](int64_t p, int64_t p1) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) at_rows[j] = rows[j];
-    if (inside) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t row = rows[j] < 0 ? 0u : (uint32_t)rows[j];
-        x[j] = *reinterpret_cast<const Row*>(a.src + (uint64_t)row * (uint32_t)a.ld + col);
-      }
-    } else {
-      // the last columns, by element: nothing behind them is read
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t row = rows[j] < 0 ? 0u : (uint32_t)rows[j];
-        const uint4 v = load8(a.src + (uint64_t)row * (uint32_t)a.ld, col, a.cols);
-        if constexpr (kWidth == 8) x[j] = v; else x[j] = make_uint2(v.x, v.y);
-      }
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t row = rows[j] < 0 ? 0u : (uint32_t)rows[j];
+      x[j] = *reinterpret_cast<const Row*>(
+          inside ? a.src + (uint64_t)row * (uint32_t)a.ld + col : a.terms_t);
     }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -145,6 +136,16 @@ __device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, 
     load(p0, p1);
     load_rows(p0 + kDepth, p1);
     for (int64_t p = p0; p < p1; p += kDepth) {
+      if (!inside) {
+        // the last columns, by element: nothing behind them is read
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t row = at_rows[j] < 0 ? 0u : (uint32_t)at_rows[j];
+          const uint4 v = load8(a.src + (uint64_t)row * (uint32_t)a.ld, col, a.cols);
+          if constexpr (kWidth == 8) x[j] = v; else x[j] = make_uint2(v.x, v.y);
+        }
+        wait_loads();
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if (at_rows[j] < 0) {

@@ -9,24 +9,31 @@ namespace {
 constexpr int kThreads = 256;
 
 // One workgroup: one tile of rows of one adapter, one piece of the
-// contraction.  Chunks of kC of it: W's chunk [rank, kC] goes through LDS (for
-// B_l [depth, rank] transposed on the way, 8 x 8 at a time), x's straight from
-// memory into the operand registers, which is each element once: a lane's
-// operand of one matrix instruction is 8 consecutive elements of its row, one
-// group of dropout's draws.  With tiles of 64 rows each wave takes 16 of
-// them, with tiles of 16 a quarter of every chunk, joined at the end.
+// contraction, in chunks of kC: the chunks of x and W go through registers
+// (two of them under way) into LDS, where the operands are read.  There x's
+// 16 bytes are one group of dropout's draws, and B_l [depth, rank] is
+// transposed, 8 rows by 4 columns at a time.  Loads are made without branches,
+// from an element that is there in place of one that is not, and cleared or
+// (the last, partial 16 bytes of a row) read again on their way into LDS: a
+// load in a branch would make the loads under way wait for each other.  With tiles of 16 rows each wave takes a quarter of
+// every chunk, joined at the end; with tiles of 64 rows 16 of them, or half
+// of them and half of a rank above 64.
 template <int kT, int kRank, bool kTransposed>
-__global__ __launch_bounds__(kThreads) void shrink_kernel(ShrinkArgs a, int tiles) {
+__global__ __launch_bounds__(kThreads, kRank <= 64 ? 3 : 2) void shrink_kernel(ShrinkArgs a, int tiles) {
   constexpr int kC = kT == 16 || kRank <= 64 ? 128 : 64;
   constexpr int kSlots = kC / 8;
   constexpr int kTiles = kRank / 16;
-  constexpr int kSteps = kT == 16 ? kC / 128 : kC / 32;   // matrix steps of a wave in a chunk
-  // pieces of W per thread and chunk: 16 bytes each, or 8 x 8 blocks
-  constexpr int kPieces = kTransposed ? kRank * kSlots / 8 : kRank * kSlots;
+  constexpr int kHalf = kT == 64 && kRank > 64 ? 2 : 1;       // parts of the rank
+  constexpr int kMine = kTiles / kHalf;                       // a wave's tiles of it
+  constexpr int kSteps = kT == 16 ? kC / 128 : kC / 32;       // its matrix steps in a chunk
+  constexpr int kX = kT * kSlots / kThreads;                  // 16-byte pieces of x per thread
+  constexpr int kPieces = kTransposed ? kRank * kSlots / 4 : kRank * kSlots;
   constexpr int kPer = (kPieces + kThreads - 1) / kThreads;
-  constexpr int kLds = kRank * kSlots > (kT == 16 ? 4 * kTiles * 64 : 0) ? kRank * kSlots
-                                                                        : 4 * kTiles * 64;
+  constexpr int kAhead = kT == 16 && kRank > 128 ? 1 : 2;     // chunks under way
+  constexpr int kJoin = kT == 16 ? 4 * kTiles * 64 : 0;
+  constexpr int kLds = (kRank + kT) * kSlots > kJoin ? (kRank + kT) * kSlots : kJoin;
   __shared__ uint4 lds[kLds];
+  uint4* xs = lds + kRank * kSlots;
   const int tile = blockIdx.z * gridDim.y + blockIdx.y, piece = blockIdx.x;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int r16 = lane & 15, g = lane >> 4;
@@ -34,87 +41,134 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(ShrinkArgs a, int tile
   const int l = a.plan.tile_adapter[tile];
   if (l < 0 || l >= a.adapters) return;
   const int rank = rank_of(a.ranks, l, a.rank);
-  const int64_t position = (int64_t)tile * kT + (kT == 16 ? 0 : wave * 16) + r16;
-  const int row = a.plan.order[position];
-  const uint16_t* src = a.src + (row < 0 ? 0 : (int64_t)row * a.ld);
+  const int64_t p0 = (int64_t)tile * kT;
   const uint16_t* w = a.w + (int64_t)l * a.rank * a.depth;
-  const int64_t draw = (int64_t)row * (a.depth / 8);       // dropout: depth % 8 == 0
 
   const int chunks = (a.depth + kC - 1) / kC;
   const int c0 = (int)((int64_t)chunks * piece / a.splits);
   const int c1 = (int)((int64_t)chunks * (piece + 1) / a.splits);
+  const int count = c1 - c0;
 
-  uint4 xr[kSteps];
-  uint4 wr[kPer][kTransposed ? 8 : 1];
-  const auto column = [&](int chunk, int s) {
-    return chunk * kC + (kT == 16 ? wave * 32 : s * 32) + 8 * g;
-  };
-  const auto load = [&](int chunk) {
+  const int xslot = tid % kSlots, xrow = tid / kSlots;
+  int row[kX];
+  const uint16_t* src[kX];
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-      xr[s] = row < 0 ? make_uint4(0, 0, 0, 0) : load8(src, column(chunk, s), a.depth);
+  for (int i = 0; i < kX; ++i) {
+    row[i] = a.plan.order[p0 + xrow + i * (kThreads / kSlots)];
+    src[i] = a.src + (row[i] < 0 ? 0u : (uint64_t)(uint32_t)row[i] * (uint32_t)a.ld);
+  }
+
+  struct Chunk {
+    uint4 x[kX];
+    uint4 w[kTransposed ? 1 : kPer];
+    uint2 t[kTransposed ? kPer : 1][8];
+  };
+  // Chunks behind the last are "loaded" too, from one address: were the loads
+  // in a branch, each wait would have to assume that none are under way.
+  const auto load = [&](int chunk, bool there, Chunk& c) {
+    const int col = chunk * kC + xslot * 8;
+    const bool whole = there && col + 8 <= a.depth;
+#pragma unroll
+    for (int i = 0; i < kX; ++i) c.x[i] = *reinterpret_cast<const uint4*>(whole ? src[i] + col : w);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int p = tid + i * kThreads;
       if constexpr (kTransposed) {
-        const int rb = p % (kRank / 8), nb = p / (kRank / 8);
-        const int at = chunk * kC + nb * 8;
+        const int rb = p % (kRank / 4) * 4, at = chunk * kC + p / (kRank / 4) % kSlots * 8;
+        const uint16_t* from = w + (rb < a.rank ? rb : 0);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          wr[i][j] = p < kPieces && at + j < a.depth && rb * 8 < rank
-                         ? clear_from(*reinterpret_cast<const uint4*>(
-                                          w + (int64_t)(at + j) * a.rank + rb * 8), rank - rb * 8)
-                         : make_uint4(0, 0, 0, 0);
+        for (int j = 0; j < 8; ++j) {
+          const int n = !there ? 0 : at + j < a.depth ? at + j : a.depth - 1;
+          c.t[i][j] = *reinterpret_cast<const uint2*>(from + (int64_t)n * a.rank);
+        }
       } else {
         const int r = p / kSlots, at = chunk * kC + p % kSlots * 8;
-        wr[i][0] = p < kPieces && r < rank ? load8(w + (int64_t)r * a.depth, at, a.depth)
-                                           : make_uint4(0, 0, 0, 0);
+        c.w[i] = *reinterpret_cast<const uint4*>(w + (int64_t)(there && r < rank ? r : 0) * a.depth +
+                                                 (there && at < a.depth ? at : 0));
+      }
+    }
+  };
+  const auto fill = [&](int chunk, Chunk& c) {
+    const int col = chunk * kC + xslot * 8;
+#pragma unroll
+    for (int i = 0; i < kX; ++i) {
+      uint4 v = c.x[i];
+      if (col + 8 > a.depth) {
+        v = load8(src[i], col, a.depth);
+        wait_loads();
+      }
+      if (!kTransposed && a.drop.threshold)
+        v = and4(v, keep_masks(block_draws((int64_t)row[i] * (a.depth / 8) + col / 8, a.drop.key),
+                               a.drop.threshold));
+      if (row[i] < 0) v = make_uint4(0, 0, 0, 0);
+      xs[lds_slot<kSlots>(xrow + i * (kThreads / kSlots), xslot)] = v;
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int p = tid + i * kThreads;
+      if (kPieces % kThreads != 0 && p >= kPieces) break;
+      if constexpr (kTransposed) {
+        const int rb = p % (kRank / 4) * 4, nb = p / (kRank / 4), at = chunk * kC + nb * 8;
+        if (at + 8 > a.depth || rb + 4 > rank) {
+          const uint32_t lo = (rank > rb ? 0xFFFFu : 0u) | (rank > rb + 1 ? 0xFFFF0000u : 0u);
+          const uint32_t hi = (rank > rb + 2 ? 0xFFFFu : 0u) | (rank > rb + 3 ? 0xFFFF0000u : 0u);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const uint32_t there = at + j < a.depth ? 0xFFFFFFFFu : 0u;
+            c.t[i][j].x &= lo & there;
+            c.t[i][j].y &= hi & there;
+          }
+        }
+        uint4 v[4];
+        transpose8x4(c.t[i], v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) lds[lds_slot<kSlots>(rb + e, nb)] = v[e];
+      } else {
+        const int r = p / kSlots, at = chunk * kC + p % kSlots * 8;
+        if (r >= rank || at >= a.depth) c.w[i] = make_uint4(0, 0, 0, 0);
+        lds[lds_slot<kSlots>(r, p % kSlots)] = c.w[i];
       }
     }
   };
 
-  f32x4 acc[kTiles];
+  f32x4 acc[kHalf][kMine];
 #pragma unroll
-  for (int i = 0; i < kTiles; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int h = 0; h < kHalf; ++h)
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) acc[h][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  // a wave's rows (kHalf tiles of 16) and its part of the rank
+  const int row0 = kT == 16 ? 0 : kHalf == 1 ? wave * 16 : (wave & 1) * 32;
+  const int rank0 = kHalf == 1 ? 0 : (wave >> 1) * (kRank / 2);
   // each tile begins elsewhere in the piece (see tile_grid on memory channels)
-  const int count = c1 - c0;
-  int chunk = c0 + (count > 0 ? tile % count : 0);
-  if (count > 0) load(chunk);
-  for (int done = 0; done < count; ++done) {
-    const int next = chunk + 1 < c1 ? chunk + 1 : c0;
-    __syncthreads();
+  const int start = count > 0 ? tile % count : 0;
+  const auto at = [&](int i) { return c0 + (start + i < count ? start + i : start + i - count); };
+  Chunk c[kAhead];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int p = tid + i * kThreads;
-      if (p >= kPieces) break;
-      if constexpr (kTransposed) {
-        const int rb = p % (kRank / 8), nb = p / (kRank / 8);
-        uint4 v[8];
-        transpose8(wr[i], v);
+  for (int i = 0; i < kAhead; ++i)
+    load(at(i), i < count, c[i]);
+  for (int done = 0; done < count; done += kAhead) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) lds[lds_slot<kSlots>(rb * 8 + c, nb)] = v[c];
-      } else {
-        lds[lds_slot<kSlots>(p / kSlots, p % kSlots)] = wr[i][0];
+    for (int b = 0; b < kAhead; ++b) {
+      const int i = done + b;
+      if (i >= count) break;
+      __syncthreads();
+      fill(at(i), c[b]);
+      __syncthreads();
+      load(at(i + kAhead), i + kAhead < count, c[b]);
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        const int slot = (kT == 16 ? wave * 4 : s * 4) + g;
+        uint4 xf[kHalf];
+#pragma unroll
+        for (int h = 0; h < kHalf; ++h) xf[h] = xs[lds_slot<kSlots>(row0 + 16 * h + r16, slot)];
+#pragma unroll
+        for (int t = 0; t < kMine; ++t) {
+          const uint4 wf = lds[lds_slot<kSlots>(rank0 + t * 16 + r16, slot)];
+#pragma unroll
+          for (int h = 0; h < kHalf; ++h) acc[h][t] = mfma16(wf, xf[h], acc[h][t]);
+        }
       }
     }
-    uint4 xf[kSteps];
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      xf[s] = xr[s];
-      if (a.drop.threshold && row >= 0)
-        xf[s] = and4(xf[s], keep_masks(block_draws(draw + column(chunk, s) / 8, a.drop.key),
-                                       a.drop.threshold));
-    }
-    __syncthreads();
-    if (done + 1 < count) load(next);
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      const int slot = (kT == 16 ? wave * 4 : s * 4) + g;
-#pragma unroll
-      for (int i = 0; i < kTiles; ++i)
-        acc[i] = mfma16(lds[lds_slot<kSlots>(i * 16 + r16, slot)], xf[s], acc[i]);
-    }
-    chunk = next;
   }
 
   float* part = a.part + (int64_t)piece * a.positions * a.rank;
@@ -122,21 +176,24 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(ShrinkArgs a, int tile
     __syncthreads();
     f32x4* sums = reinterpret_cast<f32x4*>(lds);
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) sums[(wave * kTiles + i) * 64 + lane] = acc[i];
+    for (int i = 0; i < kTiles; ++i) sums[(wave * kTiles + i) * 64 + lane] = acc[0][i];
     __syncthreads();
     for (int i = wave; i < kTiles; i += 4) {
       f32x4 v = sums[i * 64 + lane];
 #pragma unroll
       for (int q = 1; q < 4; ++q) v += sums[(q * kTiles + i) * 64 + lane];
       const int r = i * 16 + 4 * g;
-      if (r < a.rank) *reinterpret_cast<f32x4*>(part + position * a.rank + r) = v;
+      if (r < a.rank) *reinterpret_cast<f32x4*>(part + (p0 + r16) * a.rank + r) = v;
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-      const int r = i * 16 + 4 * g;
-      if (r < a.rank) *reinterpret_cast<f32x4*>(part + position * a.rank + r) = acc[i];
-    }
+    for (int h = 0; h < kHalf; ++h)
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        const int r = rank0 + i * 16 + 4 * g;
+        if (r < a.rank)
+          *reinterpret_cast<f32x4*>(part + (p0 + row0 + 16 * h + r16) * a.rank + r) = acc[h][i];
+      }
   }
 }
 
@@ -254,7 +311,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(JoinArgs a, int tile_row
 int adapter_shrink_splits(int64_t tiles, int64_t depth, int64_t rank) {
   const int64_t chunks = (depth + 127) / 128;
   if (tiles < 1) return 1;
-  int64_t s = (512 + tiles - 1) / tiles;
+  int64_t s = (768 + tiles - 1) / tiles;
   if (s > chunks / 2) s = chunks / 2;
   return s < 1 ? 1 : (int)s;
 }
