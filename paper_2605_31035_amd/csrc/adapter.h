@@ -118,14 +118,20 @@ __device__ __forceinline__ void transpose8x4(const uint2 (&v)[8], uint4 (&w)[4])
   }
 }
 
-// LDS tiles of rows of kSlots 16-byte slots: slot s of row r stands at
-// s ^ row_key(r), so that 8 consecutive rows at one slot (fragment reads) and
-// rows r, r + 8, ... at one slot (writes of transposed 8 x 8 blocks) fall
-// into different banks.
-__device__ __forceinline__ int row_key(int r) { return r ^ (r >> 3); }
+// LDS tiles of rows of kSlots 16-byte slots: slot s of row r stands at s ^
+// key(r), so that 8 consecutive rows at one slot (operand reads) fall into
+// different banks.  The key depends on r mod 16 alone, so that the tiles of
+// 16 rows differ by a constant that the read instruction adds; rows r, r + 4,
+// ... at one slot (writes of transposed 8 x 4 blocks) still meet four banks.
 template <int kSlots>
 __device__ __forceinline__ int lds_slot(int row, int slot) {
-  return row * kSlots + (slot ^ (row_key(row) & (kSlots - 1)));
+  return row * kSlots + (slot ^ ((row ^ (row >> 2 & 2)) & (kSlots - 1)));
+}
+// The same for tiles written in transposed 8 x 8 blocks: rows r, r + 8, ...
+// at one slot fall into different banks too.
+template <int kSlots>
+__device__ __forceinline__ int lds_slot8(int row, int slot) {
+  return row * kSlots + (slot ^ ((row ^ (row >> 3)) & (kSlots - 1)));
 }
 
 __device__ __forceinline__ int rank_of(const int32_t* ranks, int l, int rank) {

@@ -9,7 +9,18 @@ namespace mixfp4 {
 
 namespace {
 
-constexpr int kThreads = 256;
+// A wave takes 32 columns of a block of 128, and all rows of the tile, or half
+// of them: of a tile of 64 rows, whose sums and base would hold half of the
+// registers, so that too few waves are there to hide the memory's latency
+// (1537x4096 rank 256: 67 -> 55 us, 2048x11008 rank 64: 61 -> 59).  The input
+// gradient with a small rank gains nothing by it (its draws need more
+// registers): 8192x4096 rank 64 57 us either way.
+constexpr int threads_of(int tile_rows, int rank, bool dx) {
+  return tile_rows == 64 && (!dx || rank > 64) ? 512 : 256;
+}
+constexpr int waves_of(int tile_rows, int rank, bool dx) {
+  return tile_rows == 16 && rank > 128 ? 1 : rank <= 64 && !dx ? 4 : 2;
+}
 
 // One workgroup: one tile of rows, `width` columns, 128 at a time and 32 of
 // them per wave.  The terms of the tile stand in LDS.  W is the left operand
@@ -23,23 +34,26 @@ constexpr int kThreads = 256;
 // without branches, from a row or column that is there in place of one that
 // is not (behind the last block, from one address): with loads in a branch
 // each wait would have to assume that none are under way.  Only tiles and blocks that are not full look at each store.
-template <int kT, int kRank, bool kDx, bool kOut16, bool kAligned>
-__global__ __launch_bounds__(kThreads, kRank <= 128 ? 2 : 1) void expand_kernel(ExpandArgs a, int width, int tiles) {
+template <int kT, int kRank, bool kDx, bool kOut16, bool kAligned, bool kJoin>
+__global__ __launch_bounds__(threads_of(kT, kRank, kDx), waves_of(kT, kRank, kDx)) void expand_kernel(ExpandArgs a, int width, int tiles) {
   constexpr int kWide = kRank < 32 ? 32 : kRank;     // terms per part
   constexpr int kSteps = kWide / 32;
-  constexpr int kRows = kT / 16;
+  constexpr int kThreads = threads_of(kT, kRank, kDx);
+  constexpr bool kShared = kThreads == 512;          // two waves per 32 columns
+  constexpr int kRows = kT / 16 / (kShared ? 2 : 1); // 16-row tiles of a wave
   constexpr int kSlots = kWide / 8;
   // pieces of W per thread and block: 16 bytes of B_l, or 8 rows by 4 columns
   // of A_l
-  constexpr int kPieces = kDx ? (32 * kSlots + kThreads - 1) / kThreads : kWide / 16;
-  constexpr bool kAhead = kRank <= 128;              // registers for W of the next block
+  constexpr int kPieces = kDx ? (32 * kSlots + kThreads - 1) / kThreads : 128 * kSlots / kThreads;
+  constexpr bool kAhead = kRank <= 128 || kThreads == 512;   // registers for W of the next block
   __shared__ uint4 terms[kT * 2 * kSlots];
   __shared__ uint4 wt[128 * kSlots];
-  __shared__ f32x4 turn[4][16 * 8];
+  __shared__ f32x4 turn[kThreads / 64][16 * 8];
   __shared__ int32_t order[kT];
   const int tile = blockIdx.z * gridDim.y + blockIdx.y;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int r16 = lane & 15, g = lane >> 4;
+  const int wave_col = (wave & 3) * 32, row0 = (wave >> 2) * 32;
   if (tile >= tiles) return;
   const int l = a.plan.tile_adapter[tile];
   if (l < 0) return;
@@ -50,15 +64,19 @@ __global__ __launch_bounds__(kThreads, kRank <= 128 ? 2 : 1) void expand_kernel(
   const int begin = blockIdx.x * width;
   const int end = a.cols - begin < width ? a.cols : begin + width;
 
-  // pieces of 16 bytes of B_l: column and slot of each, the same in every block
+  // pieces of 16 bytes of B_l: column and slot of each, the same in every
+  // block; a wave loads its own 32 columns unless another shares them
   const int slots = a.rank >> 3;
+  const int p_first = kShared ? tid : lane, p_step = kShared ? kThreads : 64;
+  constexpr int kSpan = kShared ? 128 : 32;
+  const int span0 = kShared ? 0 : wave_col;
   int piece_col[kDx ? 1 : kPieces], piece_at[kDx ? 1 : kPieces];
   if constexpr (!kDx) {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int p = lane + 64 * i, col = p / slots, slot = p - col * slots;
-      piece_col[i] = col < 32 ? col : 32;
-      piece_at[i] = col < 32 ? lds_slot<kSlots>(wave * 32 + col, slot) : 0;
+      const int p = p_first + p_step * i, col = p / slots, slot = p - col * slots;
+      piece_col[i] = col < kSpan ? col : kSpan;
+      piece_at[i] = col < kSpan ? lds_slot<kSlots>(span0 + col, slot) : 0;
       if (slot * 8 >= rank) piece_col[i] |= 0x100;              // behind the adapter's rank
       else if (slot * 8 + 8 > rank) piece_col[i] |= 0x200;
     }
@@ -79,12 +97,12 @@ __global__ __launch_bounds__(kThreads, kRank <= 128 ? 2 : 1) void expand_kernel(
         }
       }
     } else {
-      // 32 columns of B_l stand side by side
-      const int c0 = block + wave * 32;
+      // columns of B_l stand side by side
+      const int c0 = block + span0;
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) {
-        const int p = lane + 64 * i;
-        const bool is = there && (piece_col[i] & 0xFF) < 32 && c0 + (piece_col[i] & 0xFF) < end;
+        const int p = p_first + p_step * i;
+        const bool is = there && (piece_col[i] & 0xFF) < kSpan && c0 + (piece_col[i] & 0xFF) < end;
         wf[i] = *reinterpret_cast<const uint4*>(w + (is ? (int64_t)c0 * a.rank + p * 8 : 0));
       }
     }
@@ -92,7 +110,47 @@ __global__ __launch_bounds__(kThreads, kRank <= 128 ? 2 : 1) void expand_kernel(
   load_w(begin, true);
 
   if (tid < kT) order[tid] = a.plan.order[p0 + tid];
-  if (rank > 0) {
+  if constexpr (kJoin) {
+    // the terms of the few rows from the pieces of their sums, sixteen reads
+    // at a time (from the first piece where there are no more)
+    const float f = none || !a.scaling ? 1.0f : a.scaling[l];
+    const int64_t size = a.positions * a.rank;
+    for (int e = tid; e < kT * kWide / 4; e += kThreads) {
+      const int q = e / (kWide / 4), r = e % (kWide / 4) * 4;
+      const int row = a.plan.order[p0 + q];
+      if (row < 0) break;                    // and all behind it
+      f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (r < rank) {
+        const float* from = a.part + (p0 + q) * a.rank + r;
+        for (int j = 0; j < a.splits; j += 16) {
+          f32x4 v[16];
+#pragma unroll
+          for (int h = 0; h < 16; ++h)
+            v[h] = *reinterpret_cast<const f32x4*>(from + (j + h < a.splits ? j + h : 0) * size);
+#pragma unroll
+          for (int h = 0; h < 16; ++h)
+            if (j + h < a.splits) sum += v[h];
+        }
+        sum *= a.z;
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+          if (r + h >= rank) sum[h] = 0.0f;
+      }
+      if (a.t && blockIdx.x == 0 && r < a.rank) {
+        float* t = a.t + (int64_t)row * a.rank + r;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) t[h] = sum[h];
+      }
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) split_bf16(f * sum[h], hi[h], lo[h]);
+      uint2* to = reinterpret_cast<uint2*>(terms);
+      to[2 * lds_slot<2 * kSlots>(q, r >> 3) + (r >> 2 & 1)] =
+          make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+      to[2 * lds_slot<2 * kSlots>(q, kSlots + (r >> 3)) + (r >> 2 & 1)] =
+          make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+    }
+  } else if (rank > 0) {
     const uint4* from = reinterpret_cast<const uint4*>(a.terms + p0 * 2 * kWide);
 #pragma unroll
     for (int i = 0; i < (kT * 2 * kSlots + kThreads - 1) / kThreads; ++i) {
@@ -112,14 +170,14 @@ __global__ __launch_bounds__(kThreads, kRank <= 128 ? 2 : 1) void expand_kernel(
   constexpr int kLoads = kAligned ? 2 * kRows : 8 * kRows;
   constexpr int kLanes = kAligned ? 8 : 32;
   const int sub = lane / kLanes, lane_col = lane % kLanes * (kAligned ? 4 : 1);
-  const bool whole = order[kT - 1] >= 0;
-  const auto row_of = [&](int i) { return order[i * (64 / kLanes) + sub]; };
+  const bool whole = order[kT - 1] >= 0;      // rows are missing at the end only
+  const auto row_of = [&](int i) { return order[row0 + i * (64 / kLanes) + sub]; };
   f32x4 base[kRows][2];
   const float* base_at = a.base ? a.base : reinterpret_cast<const float*>(a.w);
   const bool has_base = a.base != nullptr;
   const auto load_base = [&](int block, bool there) {
     there = there && has_base;
-    int col = block + wave * 32 + lane_col;
+    int col = block + wave_col + lane_col;
     col = col < end ? col : end - (kAligned ? 4 : 1);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -138,7 +196,7 @@ __global__ __launch_bounds__(kThreads, kRank <= 128 ? 2 : 1) void expand_kernel(
   const auto run = [&](auto check) {
     constexpr bool kCheck = decltype(check)::value;
     for (int block = begin; block < end; block += 128) {
-      const int c0 = block + wave * 32;
+      const int c0 = block + wave_col;
       const bool more = block + 128 < end;
       f32x4 acc[kRows][2];
 #pragma unroll
@@ -161,6 +219,7 @@ __global__ __launch_bounds__(kThreads, kRank <= 128 ? 2 : 1) void expand_kernel(
         }
         __syncthreads();
       } else {
+        if (kShared && block > begin) __syncthreads();
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
@@ -169,9 +228,10 @@ __global__ __launch_bounds__(kThreads, kRank <= 128 ? 2 : 1) void expand_kernel(
             if (piece_col[i] & 0x100) v = make_uint4(0, 0, 0, 0);
             if (piece_col[i] & 0x200) v = clear_from(v, rank & 7);
           }
-          if ((piece_col[i] & 0xFF) < 32) wt[piece_at[i]] = v;
+          if ((piece_col[i] & 0xFF) < kSpan) wt[piece_at[i]] = v;
         }
         __builtin_amdgcn_wave_barrier();
+        if (kShared) __syncthreads();
       }
       if (kAhead) load_w(block + 128, more);
 #pragma unroll
@@ -180,11 +240,11 @@ __global__ __launch_bounds__(kThreads, kRank <= 128 ? 2 : 1) void expand_kernel(
         uint4 f[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-          f[j] = wt[lds_slot<kSlots>(wave * 32 + 8 * (r16 >> 2) + 4 * j + (r16 & 3), 4 * s + g)];
+          f[j] = wt[lds_slot<kSlots>(wave_col + 8 * (r16 >> 2) + 4 * j + (r16 & 3), 4 * s + g)];
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-          const uint4 hi = terms[lds_slot<2 * kSlots>(i * 16 + r16, 4 * s + g)];
-          const uint4 lo = terms[lds_slot<2 * kSlots>(i * 16 + r16, kSlots + 4 * s + g)];
+          const uint4 hi = terms[lds_slot<2 * kSlots>(row0 + i * 16 + r16, 4 * s + g)];
+          const uint4 lo = terms[lds_slot<2 * kSlots>(row0 + i * 16 + r16, kSlots + 4 * s + g)];
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             acc[i][j] = mfma16(f[j], lo, acc[i][j]);
@@ -197,7 +257,7 @@ __global__ __launch_bounds__(kThreads, kRank <= 128 ? 2 : 1) void expand_kernel(
       for (int i = 0; i < kRows; ++i) {
         if constexpr (kDx) {
           if (a.drop.threshold) {
-            const int row = order[i * 16 + r16], col = c0 + 8 * g;
+            const int row = order[row0 + i * 16 + r16], col = c0 + 8 * g;
             const uint4 d = block_draws((int64_t)row * (a.cols / 8) + col / 8, a.drop.key);
             const uint32_t u[4] = {d.x, d.y, d.z, d.w};
 #pragma unroll
@@ -254,39 +314,70 @@ __global__ __launch_bounds__(kThreads, kRank <= 128 ? 2 : 1) void expand_kernel(
     run(std::true_type{});
 }
 
-template <int kT, bool kDx, bool kOut16, bool kAligned>
+template <int kT, bool kDx, bool kOut16, bool kAligned, bool kJoin = false>
 void launch(const ExpandArgs& a, int64_t tiles, int width, hipStream_t stream) {
   const dim3 grid = tile_grid((a.cols + width - 1) / width, tiles);
   const int n = (int)tiles;
+  const auto go = [&](auto rank) {
+    constexpr int kRank = decltype(rank)::value;
+    expand_kernel<kT, kRank, kDx, kOut16, kAligned, kJoin>
+        <<<grid, threads_of(kT, kRank, kDx), 0, stream>>>(a, width, n);
+  };
   switch (padded_rank(a.rank)) {
-    case 16: expand_kernel<kT, 16, kDx, kOut16, kAligned><<<grid, kThreads, 0, stream>>>(a, width, n); break;
-    case 32: expand_kernel<kT, 32, kDx, kOut16, kAligned><<<grid, kThreads, 0, stream>>>(a, width, n); break;
-    case 64: expand_kernel<kT, 64, kDx, kOut16, kAligned><<<grid, kThreads, 0, stream>>>(a, width, n); break;
-    case 128: expand_kernel<kT, 128, kDx, kOut16, kAligned><<<grid, kThreads, 0, stream>>>(a, width, n); break;
-    default: expand_kernel<kT, 256, kDx, kOut16, kAligned><<<grid, kThreads, 0, stream>>>(a, width, n); break;
+    case 16: go(std::integral_constant<int, 16>{}); break;
+    case 32: go(std::integral_constant<int, 32>{}); break;
+    case 64: go(std::integral_constant<int, 64>{}); break;
+    case 128: go(std::integral_constant<int, 128>{}); break;
+    default: go(std::integral_constant<int, 256>{}); break;
   }
 }
 
 template <int kT, bool kDx, bool kOut16>
 void launch(const ExpandArgs& a, int64_t tiles, int width, bool aligned, hipStream_t stream) {
+  if constexpr (kT == 16 && !kDx) {
+    if (a.part) {
+      aligned ? launch<kT, kDx, kOut16, true, true>(a, tiles, width, stream)
+              : launch<kT, kDx, kOut16, false, true>(a, tiles, width, stream);
+      return;
+    }
+  }
   aligned ? launch<kT, kDx, kOut16, true>(a, tiles, width, stream)
           : launch<kT, kDx, kOut16, false>(a, tiles, width, stream);
 }
 
 }  // namespace
 
+// Whether the wide product joins the pieces itself: every workgroup of a tile
+// then reads them, which beats the join's launch (4.7 us) as long as that is
+// little, up to 4 MB in all (17 MB cost 6.6 us).
+bool adapter_expand_joins(int64_t m, int64_t n, int64_t rank, int tile_rows, int splits) {
+  return tile_rows == 16 && (n + 127) / 128 * m * rank * 4 * splits <= (int64_t(4) << 20);
+}
+
 hipError_t launch_adapter_expand(const ExpandArgs& a, int tile_rows, int64_t tiles, bool dx,
                                  bool out16, hipStream_t stream) {
-  // columns per workgroup: wide enough that the terms are read seldom, as
-  // long as the device stays full
-  const int padded = padded_rank(a.rank);
-  int64_t width = a.cols * tiles / 3072;
-  if (width > 5 * padded) width = 5 * padded;
-  width = (width + 127) / 128 * 128;
-  if (width < 128) width = 128;
+  // Blocks of 128 columns per workgroup: several, so that the terms are read
+  // seldom and a block's memory is requested under the one before, as long as
+  // the device stays full.  A rank above 128 leaves room for one workgroup per
+  // compute unit: as many as there are units (1537x4096 rank 256: 55 us with
+  // one block each, 46 with four, 49 with five).  Else two (8192x14336 rank 64:
+  // 200 us with one, 191 with two, 204 with three), one below 3072 workgroups
+  // (2048x11008: the same with one to three); the input gradient pays more for
+  // a workgroup's start (8192x4096: 62 us with one, 56 with two).  Tiles of 16
+  // rows: 1024 workgroups (48x11008 rank 64: 22 us with one, 19 with three).
+  const bool small = tile_rows == 16;
+  const int64_t blocks = (a.cols + 127) / 128, units = blocks * tiles;
+  int64_t w;
+  if (small)
+    w = units / 1024 < 4 ? units / 1024 : 4;
+  else if (padded_rank(a.rank) > 128)
+    w = (units + compute_units() - 1) / compute_units();
+  else
+    w = (dx ? units + 3071 : units) / 3072 < 2 ? 1 : 2;
+  if (w > 8) w = 8;
+  const int64_t width = 128 * (w < 1 ? 1 : w);
   const bool aligned = a.cols % 4 == 0 && ((uintptr_t)a.out & (out16 ? 7 : 15)) == 0 && a.ldo % 4 == 0 &&
                        (!a.base || (((uintptr_t)a.base & 15) == 0 && a.ldb % 4 == 0));
-  const bool small = tile_rows == 16;
   const int wd = (int)width;
   if (dx) {
     small ? launch<16, true, false>(a, tiles, wd, aligned, stream)

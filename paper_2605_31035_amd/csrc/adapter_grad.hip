@@ -56,6 +56,10 @@ __device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, 
   f32x4 acc[kTiles][kSide];
   const int wave_col = wave * 16 * kSide;
   const auto store = [&](float* to) {
+    // opaque, so that the addresses are made here and not kept in registers
+    // over the steps
+    int r16 = lane & 15, g = lane >> 4;
+    asm volatile("" : "+v"(r16), "+v"(g));
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
       if constexpr (kDb) {
@@ -166,12 +170,12 @@ __device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, 
         uint4 v[8];
         transpose8(x, v);
 #pragma unroll
-        for (int c = 0; c < 8; ++c) xt[lds_slot<kSlots>(cg * 8 + c, pg)] = v[c];
+        for (int c = 0; c < 8; ++c) xt[lds_slot8<kSlots>(cg * 8 + c, pg)] = v[c];
       } else {
         uint4 v[4];
         transpose8x4(x, v);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) xt[lds_slot<kSlots>(cg * 4 + c, pg)] = v[c];
+        for (int c = 0; c < 4; ++c) xt[lds_slot8<kSlots>(cg * 4 + c, pg)] = v[c];
       }
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
@@ -191,7 +195,7 @@ __device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, 
 #pragma unroll
         for (int j = 0; j < kSide; ++j) {
           const int c = kDb ? 16 * j + r16 : 32 * (j >> 1) + 8 * (r16 >> 2) + 4 * (j & 1) + (r16 & 3);
-          xf[j] = xt[lds_slot<kSlots>(wave_col + c, 4 * s + g)];
+          xf[j] = xt[lds_slot8<kSlots>(wave_col + c, 4 * s + g)];
         }
 #pragma unroll
         for (int i = 0; i < kTiles; ++i)
@@ -266,7 +270,7 @@ int adapter_grad_splits(int64_t m, int64_t n, int64_t k, int64_t rank) {
   const int64_t blocks = (blocks_of(n, rank) + blocks_of(k, rank)) * (rank > 128 ? 2 : 1), round = 2 * compute_units();
   int best = 1;
   double score = 0.0;
-  for (int64_t s = 1; s <= 64 && (s == 1 || s * 256 <= m); ++s) {
+  for (int64_t s = 1; s <= 64 && (s == 1 || s * 64 <= m); ++s) {
     const int64_t groups = blocks * s;
     const double full = (double)groups / (double)((groups + round - 1) / round * round);
     const double v = full / (1.0 + (s > 1 ? (double)(s * rank * 4) / (double)m : 0.0));

@@ -66,15 +66,22 @@ hipError_t launch_adapter(const AdapterArgs& a, hipStream_t stream) {
       {a.x, a.ldx, a.a, a.ranks, a.plan, a.drop, (int)a.k, rank, adapters, p.splits, p.positions, p.part},
       p.tile_rows, p.tiles, false, stream);
   if (e != hipSuccess) return e;
-  JoinArgs j{};
-  j.part = p.part, j.scaling = a.scaling, j.ranks = a.ranks, j.plan = a.plan;
-  j.positions = p.positions, j.rank = rank, j.adapters = adapters, j.splits = p.splits;
-  j.z = a.drop.z, j.terms = p.terms, j.t = a.t;
-  e = launch_adapter_join(j, p.tile_rows, stream);
-  if (e != hipSuccess) return e;
-  return launch_adapter_expand({p.terms, a.b, a.ranks, a.plan, {}, a.c, a.ldc, a.out, a.ldo, (int)a.n,
-                                rank, adapters},
-                               p.tile_rows, p.tiles, false, a.out16, stream);
+  ExpandArgs x{};
+  x.w = a.b, x.ranks = a.ranks, x.plan = a.plan, x.base = a.c, x.ldb = a.ldc, x.out = a.out;
+  x.ldo = a.ldo, x.cols = (int)a.n, x.rank = rank, x.adapters = adapters;
+  if (adapter_expand_joins(a.m, a.n, rank, p.tile_rows, p.splits)) {
+    x.part = p.part, x.scaling = a.scaling, x.t = a.t;
+    x.positions = p.positions, x.splits = p.splits, x.z = a.drop.z;
+  } else {
+    JoinArgs j{};
+    j.part = p.part, j.scaling = a.scaling, j.ranks = a.ranks, j.plan = a.plan;
+    j.positions = p.positions, j.rank = rank, j.adapters = adapters, j.splits = p.splits;
+    j.z = a.drop.z, j.terms = p.terms, j.t = a.t;
+    e = launch_adapter_join(j, p.tile_rows, stream);
+    if (e != hipSuccess) return e;
+    x.terms = p.terms;
+  }
+  return launch_adapter_expand(x, p.tile_rows, p.tiles, false, a.out16, stream);
 }
 
 hipError_t launch_adapter_backward(const AdapterArgs& a, hipStream_t stream) {
@@ -94,9 +101,11 @@ hipError_t launch_adapter_backward(const AdapterArgs& a, hipStream_t stream) {
   j.z = a.drop.z, j.terms = p.terms, j.terms_t = p.terms_t, j.t_in = a.t, j.t_in_t = p.t_t;
   e = launch_adapter_join(j, p.tile_rows, stream);
   if (e != hipSuccess) return e;
-  e = launch_adapter_expand({p.terms, a.a, a.ranks, a.plan, a.drop, a.dx0, a.lddx0, a.dx, a.lddx,
-                             (int)a.k, rank, adapters},
-                            p.tile_rows, p.tiles, true, false, stream);
+  ExpandArgs x{};
+  x.terms = p.terms, x.w = a.a, x.ranks = a.ranks, x.plan = a.plan, x.drop = a.drop;
+  x.base = a.dx0, x.ldb = a.lddx0, x.out = a.dx, x.ldo = a.lddx;
+  x.cols = (int)a.k, x.rank = rank, x.adapters = adapters;
+  e = launch_adapter_expand(x, p.tile_rows, p.tiles, true, false, stream);
   if (e != hipSuccess) return e;
   return launch_adapter_grad(grad, stream);
 }

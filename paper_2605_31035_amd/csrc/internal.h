@@ -357,7 +357,16 @@ struct ExpandArgs {
   void* out;
   int64_t ldo;
   int cols, rank, adapters;
+  // Tiles of 16 rows, not dx: the pieces themselves in place of `terms`
+  // (unless NULL), with the join's factor and t.
+  const float* part;
+  const float* scaling;
+  float* t;
+  int64_t positions;
+  int splits;
+  float z;
 };
+bool adapter_expand_joins(int64_t m, int64_t n, int64_t rank, int tile_rows, int splits);
 hipError_t launch_adapter_expand(const ExpandArgs& a, int tile_rows, int64_t tiles, bool dx,
                                  bool out16, hipStream_t stream);
 // dA_l [rank, k] (src = x with dropout, terms of u) and dB_l [n, rank] (src =
