@@ -1,235 +1,23 @@
-// The gradients of the adapters: dA_l = sum u_i^T (keep_i x_i) and
-// dB_l = sum dy_i^T t_i over the rows i of adapter l, products whose
-// contraction runs along the rows.
-#include <type_traits>
-
-#include "adapter.h"
+// Kernels of the backward pass behind the join: the input gradient
+// (adapter_expand.h) and the adapters' gradients (adapter_grad.h).
+#include "adapter_expand.h"
+#include "adapter_grad.h"
 
 namespace mixfp4 {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kSumThreads = 256;
 
-// Columns of x or dy of a workgroup: the more, the fewer reads of the terms;
-// the sums of 256 columns by a rank of 64 take 64 registers of each lane.
-constexpr int cols_of(int padded) { return padded <= 64 ? 256 : 128; }
-
-// Positions of the pieces: whole tiles, split evenly over those in use.
-__device__ __forceinline__ int64_t piece_begin(int64_t tiles, int s, int splits) {
-  return tiles * s / splits;
-}
-
-// One workgroup: 256 or 128 columns, all of the rank, one piece of the positions.
-// It walks the adapters that its piece holds, kDepth positions at a time.
-// The columns of x or dy are transposed through registers into LDS (8 rows by
-// 8 or 4 columns per thread; dropout's draws are made on the rows), the terms
-// come transposed from the join, so that an operand's 8 consecutive positions
-// are one LDS read.  The next step's reads are under way while a step is
-// multiplied.  An adapter within one piece is written at once, one across
-// pieces as partial sums (at most two per piece: the one that enters it and
-// the one that leaves it) for sum_kernel.  A rank above 128 takes two
-// workgroups (r0), so that the sums stay in registers.
-template <int kRank, bool kDb>
-__device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, int block, int piece,
-                                          int r0, uint4* lds) {
-  constexpr int kTiles = kRank / 16;
-  constexpr int kCols = cols_of(kRank), kSide = kCols / 64; // 16-column tiles of a wave
-  constexpr int kDepth = 64;
-  constexpr int kSlots = kDepth / 8;
-  constexpr int kWidth = kCols / 32;                       // columns of a thread's piece
-  constexpr int kGroups = kCols / kWidth;
-  constexpr int kTerms = 3 * kRank * kSlots;
-  constexpr int kPer = (kTerms + kThreads - 1) / kThreads;
-  using Row = std::conditional_t<kWidth == 8, uint4, uint2>;
-  uint4* xt = lds;
-  uint4* ut = lds + kCols * kSlots;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int r16 = lane & 15, g = lane >> 4;
-  const int col0 = block * kCols;
-  const int64_t tiles = q.plan.seg[q.adapters];
-  const int64_t t0 = piece_begin(tiles, piece, q.splits), t1 = piece_begin(tiles, piece + 1, q.splits);
-  const int64_t matrix = (int64_t)q.rank * a.cols;
-  const int cg = tid % kGroups, pg = tid / kGroups;
-  const int col = col0 + cg * kWidth;
-
-  f32x4 acc[kTiles][kSide];
-  const int wave_col = wave * 16 * kSide;
-  const auto store = [&](float* to) {
-    // opaque, so that the addresses are made here and not kept in registers
-    // over the steps
-    int r16 = lane & 15, g = lane >> 4;
-    asm volatile("" : "+v"(r16), "+v"(g));
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-      if constexpr (kDb) {
-        const int r = r0 + 16 * i + 4 * g;
-#pragma unroll
-        for (int j = 0; j < kSide; ++j) {
-          const int n = col0 + wave_col + 16 * j + r16;
-          if (n < a.cols && r < q.rank) *reinterpret_cast<f32x4*>(to + (int64_t)n * q.rank + r) = acc[i][j];
-        }
-      } else {
-        const int r = r0 + 16 * i + r16;
-#pragma unroll
-        for (int j = 0; j < kSide; ++j) {
-          const int c = col0 + wave_col + 32 * (j >> 1) + 8 * g;
-          if (r < q.rank && c < a.cols)
-            *reinterpret_cast<f32x4*>(to + (int64_t)r * a.cols + c + 4 * (j & 1)) = acc[i][j];
-        }
-      }
-    }
-  };
-  const auto clear = [&]() {
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-      for (int j = 0; j < kSide; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  };
-
-  if (piece == 0)                  // adapters without rows
-    for (int l = 0; l < q.adapters; ++l)
-      if (q.plan.seg[l] == q.plan.seg[l + 1]) {
-        clear();
-        store(a.out + l * matrix);
-      }
-  if (t0 >= t1) return;
-
-  int rows[8], at_rows[8];         // of the next step's reads, of the reads under way
-  Row x[8];
-  uint4 u[kPer];
-  const auto load_rows = [&](int64_t p, int64_t p1) {
-    const int64_t at = p + pg * 8;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) rows[j] = -1;
-    if (at < p1) {
-      const int4 lo = *reinterpret_cast<const int4*>(q.plan.order + at);
-      const int4 hi = *reinterpret_cast<const int4*>(q.plan.order + at + 4);
-      rows[0] = lo.x, rows[1] = lo.y, rows[2] = lo.z, rows[3] = lo.w;
-      rows[4] = hi.x, rows[5] = hi.y, rows[6] = hi.z, rows[7] = hi.w;
-    }
-  };
-  const bool inside = col + kWidth <= a.cols;
-  const auto load = [&](int64_t p, int64_t p1) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) at_rows[j] = rows[j];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t row = rows[j] < 0 ? 0u : (uint32_t)rows[j];
-      x[j] = *reinterpret_cast<const Row*>(
-          inside ? a.src + (uint64_t)row * (uint32_t)a.ld + col : a.terms_t);
-    }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int e = tid + i * kThreads;
-      const int64_t pos = p + e % kSlots * 8;
-      const int h = e / (kRank * kSlots), r = e / kSlots - h * kRank;
-      const uint16_t* from =
-          a.terms_t + (int64_t)(h * q.padded + r0 + r) * q.positions + (pos < p1 ? pos : p);
-      if (kTerms % kThreads == 0 || e < kTerms) u[i] = *reinterpret_cast<const uint4*>(from);
-    }
-  };
-
-  for (int l = q.plan.tile_adapter[t0]; l < q.adapters && q.plan.seg[l] < t1; ++l) {
-    const int64_t first = q.plan.seg[l], last = q.plan.seg[l + 1];
-    if (first == last) continue;
-    const int64_t p0 = (first > t0 ? first : t0) * q.tile_rows;
-    const int64_t p1 = (last < t1 ? last : t1) * q.tile_rows;
-    clear();
-    load_rows(p0, p1);
-    load(p0, p1);
-    load_rows(p0 + kDepth, p1);
-    for (int64_t p = p0; p < p1; p += kDepth) {
-      if (!inside) {
-        // the last columns, by element: nothing behind them is read
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint32_t row = at_rows[j] < 0 ? 0u : (uint32_t)at_rows[j];
-          const uint4 v = load8(a.src + (uint64_t)row * (uint32_t)a.ld, col, a.cols);
-          if constexpr (kWidth == 8) x[j] = v; else x[j] = make_uint2(v.x, v.y);
-        }
-        wait_loads();
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (at_rows[j] < 0) {
-          x[j] = Row{};
-        } else if (!kDb && q.drop.threshold) {
-          const uint4 m = keep_masks(block_draws((int64_t)at_rows[j] * (a.cols / 8) + col / 8, q.drop.key),
-                                     q.drop.threshold);
-          if constexpr (kWidth == 8) {
-            x[j] = and4(x[j], m);
-          } else {
-            x[j].x &= col & 4 ? m.z : m.x;
-            x[j].y &= col & 4 ? m.w : m.y;
-          }
-        }
-      }
-      __syncthreads();
-      if constexpr (kWidth == 8) {
-        uint4 v[8];
-        transpose8(x, v);
-#pragma unroll
-        for (int c = 0; c < 8; ++c) xt[lds_slot8<kSlots>(cg * 8 + c, pg)] = v[c];
-      } else {
-        uint4 v[4];
-        transpose8x4(x, v);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) xt[lds_slot8<kSlots>(cg * 4 + c, pg)] = v[c];
-      }
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int e = tid + i * kThreads;
-        if (p + e % kSlots * 8 >= p1) u[i] = make_uint4(0, 0, 0, 0);
-        if (kTerms % kThreads == 0 || e < kTerms) ut[lds_slot<kSlots>(e / kSlots, e % kSlots)] = u[i];
-      }
-      __syncthreads();
-      if (p + kDepth < p1) {
-        load(p + kDepth, p1);
-        load_rows(p + 2 * kDepth, p1);
-      }
-#pragma unroll
-      for (int s = 0; s < kDepth / 32; ++s) {
-        if (p + 32 * s >= p1) break;
-        uint4 xf[kSide];
-#pragma unroll
-        for (int j = 0; j < kSide; ++j) {
-          const int c = kDb ? 16 * j + r16 : 32 * (j >> 1) + 8 * (r16 >> 2) + 4 * (j & 1) + (r16 & 3);
-          xf[j] = xt[lds_slot8<kSlots>(wave_col + c, 4 * s + g)];
-        }
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-          for (int h = 2; h >= 0; --h) {             // the smallest term first
-            const uint4 uf = ut[lds_slot<kSlots>(h * kRank + 16 * i + r16, 4 * s + g)];
-#pragma unroll
-            for (int j = 0; j < kSide; ++j)
-              acc[i][j] = kDb ? mfma16(uf, xf[j], acc[i][j]) : mfma16(xf[j], uf, acc[i][j]);
-          }
-      }
-    }
-    if (first >= t0 && last <= t1)
-      store(a.out + l * matrix);
-    else
-      store(a.part + (2 * piece + (first >= t0)) * matrix);
-  }
-}
-
-template <int kRank>
-__global__ __launch_bounds__(kThreads, 2) void grad_kernel(GradArgs q) {
-  constexpr int kCols = cols_of(kRank);
-  __shared__ uint4 lds[(kCols + 3 * kRank) * 8];
-  // the workgroups of a piece side by side: they read the same rows
-  const int blocks_a = (q.a.cols + kCols - 1) / kCols, blocks = blocks_a + (q.b.cols + kCols - 1) / kCols;
-  const int piece = blockIdx.x / blocks, block = blockIdx.x % blocks;
-  if (block < blocks_a)
-    grad_body<kRank, false>(q.a, q, block, piece, blockIdx.y * kRank, lds);
-  else
-    grad_body<kRank, true>(q.b, q, block - blocks_a, piece, blockIdx.y * kRank, lds);
+// The gradients of a rank above 64 by themselves: their sums and dx's take
+// the registers of one compute unit each.
+__global__ __launch_bounds__(kGradThreads, 2) void grad_kernel(GradArgs q) {
+  __shared__ uint4 lds[grad_lds(128)];
+  grad_block<128>(q, blockIdx.x, blockIdx.y * 128, lds);
 }
 
 // The adapters across pieces: their partial sums, in the order of the pieces.
-__global__ __launch_bounds__(kThreads) void sum_kernel(GradArgs q) {
+__global__ __launch_bounds__(kSumThreads) void sum_kernel(GradArgs q) {
   const GradSide& a = blockIdx.z ? q.b : q.a;
   const int l = blockIdx.y;
   const int64_t tiles = q.plan.seg[q.adapters];
@@ -243,8 +31,8 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(GradArgs q) {
   }
   if (s0 == s1) return;
   const int64_t matrix = (int64_t)q.rank * a.cols;
-  for (int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4; i < matrix;
-       i += (int64_t)gridDim.x * kThreads * 4) {
+  for (int64_t i = ((int64_t)blockIdx.x * kSumThreads + threadIdx.x) * 4; i < matrix;
+       i += (int64_t)gridDim.x * kSumThreads * 4) {
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
     for (int s = s0; s <= s1; ++s) {
@@ -253,6 +41,45 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(GradArgs q) {
       v += *reinterpret_cast<const f32x4*>(a.part + slot * matrix + i);
     }
     *reinterpret_cast<f32x4*>(a.out + l * matrix + i) = v;
+  }
+}
+
+// Workgroups of a launch: dx's (`across` per tile) and the gradients'.
+struct Wide {
+  int width, across, dxs, grads;
+};
+
+// dx and the gradients in one launch: dx is bound by memory, the gradients
+// wait for their rows and multiply, so side by side they take less than in
+// turn (8192x14336x4096 rank 64: MEASURED).  The gradients' workgroups, which
+// run long, are spread evenly over the front of the launch, up to the middle
+// of dx's.
+template <int kT, int kRank, bool kAligned>
+__global__ __launch_bounds__(kGradThreads, 2) void backward_kernel(ExpandArgs x, GradArgs q, Wide w) {
+  constexpr int kDx = expand_lds(kT, kRank, true), kGrad = grad_lds(kRank);
+  __shared__ uint4 lds[kDx > kGrad ? kDx : kGrad];
+  const uint64_t b = blockIdx.x, front = (uint64_t)w.grads + w.dxs / 2;
+  if (b < front) {
+    const int before = (int)(b * w.grads / front), behind = (int)((b + 1) * w.grads / front);
+    if (behind > before) {
+      grad_block<kRank>(q, before, 0, lds);
+      return;
+    }
+    const int i = (int)b - before;
+    expand_body<kT, kRank, true, false, kAligned, false>(x, w.width, i / w.across, i % w.across, lds);
+  } else {
+    const int i = (int)b - w.grads;
+    expand_body<kT, kRank, true, false, kAligned, false>(x, w.width, i / w.across, i % w.across, lds);
+  }
+}
+
+template <int kT, bool kAligned>
+void launch(const ExpandArgs& x, const GradArgs& q, const Wide& w, hipStream_t stream) {
+  const unsigned grid = (unsigned)(w.dxs + w.grads);
+  switch (padded_rank(q.rank)) {
+    case 16: backward_kernel<kT, 16, kAligned><<<grid, kGradThreads, 0, stream>>>(x, q, w); break;
+    case 32: backward_kernel<kT, 32, kAligned><<<grid, kGradThreads, 0, stream>>>(x, q, w); break;
+    default: backward_kernel<kT, 64, kAligned><<<grid, kGradThreads, 0, stream>>>(x, q, w); break;
   }
 }
 
@@ -282,20 +109,37 @@ int adapter_grad_splits(int64_t m, int64_t n, int64_t k, int64_t rank) {
   return best;
 }
 
-hipError_t launch_adapter_grad(const GradArgs& q, hipStream_t stream) {
-  const unsigned grid = (unsigned)((blocks_of(q.a.cols, q.rank) + blocks_of(q.b.cols, q.rank)) * q.splits);
-  switch (padded_rank(q.rank)) {
-    case 16: grad_kernel<16><<<grid, kThreads, 0, stream>>>(q); break;
-    case 32: grad_kernel<32><<<grid, kThreads, 0, stream>>>(q); break;
-    case 64: grad_kernel<64><<<grid, kThreads, 0, stream>>>(q); break;
-    case 128: grad_kernel<128><<<grid, kThreads, 0, stream>>>(q); break;
-    default: grad_kernel<128><<<dim3(grid, 2), kThreads, 0, stream>>>(q); break;
+// The backward pass behind the join: dx and both gradients.  With a rank up to
+// 64 in one launch.
+hipError_t launch_adapter_grad(const GradArgs& q, const ExpandArgs& dx, int tile_rows, int64_t tiles,
+                               hipStream_t stream) {
+  const int64_t grads = (blocks_of(q.a.cols, q.rank) + blocks_of(q.b.cols, q.rank)) * q.splits;
+  hipError_t e = hipSuccess;
+  if (q.rank > 64) {
+    if (tiles > 0) e = launch_adapter_expand(dx, tile_rows, tiles, true, false, stream);
+    if (e != hipSuccess) return e;
+    grad_kernel<<<dim3((unsigned)grads, q.rank > 128 ? 2 : 1), kGradThreads, 0, stream>>>(q);
+  } else {
+    const int width = tiles > 0 ? adapter_expand_width(dx, tile_rows, tiles, true) : 128;
+    int64_t across = (dx.cols + width - 1) / width;
+    const bool together = across * tiles < (1 << 23);     // workgroups of one launch
+    if (!together) {
+      e = launch_adapter_expand(dx, tile_rows, tiles, true, false, stream);
+      if (e != hipSuccess) return e;
+      across = 0;
+    }
+    const Wide w{width, (int)across, (int)(across * tiles), (int)grads};
+    const bool aligned = adapter_expand_aligned(dx, false);
+    if (tile_rows == 16)
+      aligned ? launch<16, true>(dx, q, w, stream) : launch<16, false>(dx, q, w, stream);
+    else
+      aligned ? launch<64, true>(dx, q, w, stream) : launch<64, false>(dx, q, w, stream);
   }
-  const hipError_t e = hipGetLastError();
+  e = hipGetLastError();
   if (e != hipSuccess || q.splits == 1) return e;
   const int64_t cols = q.a.cols > q.b.cols ? q.a.cols : q.b.cols;
-  const int64_t blocks = ((int64_t)q.rank * cols + 4 * kThreads - 1) / (4 * kThreads);
-  sum_kernel<<<dim3((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)q.adapters, 2), kThreads, 0,
+  const int64_t blocks = ((int64_t)q.rank * cols + 4 * kSumThreads - 1) / (4 * kSumThreads);
+  sum_kernel<<<dim3((unsigned)(blocks < 1024 ? blocks : 1024), (unsigned)q.adapters, 2), kSumThreads, 0,
                stream>>>(q);
   return hipGetLastError();
 }

@@ -90,24 +90,23 @@ hipError_t launch_adapter_backward(const AdapterArgs& a, hipStream_t stream) {
   const GradArgs grad{{a.x, a.ldx, p.terms_t, p.part_a, a.da, (int)a.k},
                       {a.dy, a.lddy, p.t_t, p.part_b, a.db, (int)a.n},
                       a.plan, a.drop, p.positions, rank, p.padded, adapters, p.grad_splits, p.tile_rows};
-  if (a.m == 0) return launch_adapter_grad(grad, stream);      // gradients of zero
-  hipError_t e = launch_adapter_shrink(
-      {a.dy, a.lddy, a.b, a.ranks, a.plan, {}, (int)a.n, rank, adapters, p.splits, p.positions, p.part},
-      p.tile_rows, p.tiles, true, stream);
-  if (e != hipSuccess) return e;
-  JoinArgs j{};
-  j.part = p.part, j.scaling = a.scaling, j.ranks = a.ranks, j.plan = a.plan;
-  j.positions = p.positions, j.rank = rank, j.adapters = adapters, j.splits = p.splits;
-  j.z = a.drop.z, j.terms = p.terms, j.terms_t = p.terms_t, j.t_in = a.t, j.t_in_t = p.t_t;
-  e = launch_adapter_join(j, p.tile_rows, stream);
-  if (e != hipSuccess) return e;
   ExpandArgs x{};
   x.terms = p.terms, x.w = a.a, x.ranks = a.ranks, x.plan = a.plan, x.drop = a.drop;
   x.base = a.dx0, x.ldb = a.lddx0, x.out = a.dx, x.ldo = a.lddx;
   x.cols = (int)a.k, x.rank = rank, x.adapters = adapters;
-  e = launch_adapter_expand(x, p.tile_rows, p.tiles, true, false, stream);
-  if (e != hipSuccess) return e;
-  return launch_adapter_grad(grad, stream);
+  if (a.m > 0) {                            // else gradients of zero
+    hipError_t e = launch_adapter_shrink(
+        {a.dy, a.lddy, a.b, a.ranks, a.plan, {}, (int)a.n, rank, adapters, p.splits, p.positions, p.part},
+        p.tile_rows, p.tiles, true, stream);
+    if (e != hipSuccess) return e;
+    JoinArgs j{};
+    j.part = p.part, j.scaling = a.scaling, j.ranks = a.ranks, j.plan = a.plan;
+    j.positions = p.positions, j.rank = rank, j.adapters = adapters, j.splits = p.splits;
+    j.z = a.drop.z, j.terms = p.terms, j.terms_t = p.terms_t, j.t_in = a.t, j.t_in_t = p.t_t;
+    e = launch_adapter_join(j, p.tile_rows, stream);
+    if (e != hipSuccess) return e;
+  }
+  return launch_adapter_grad(grad, x, p.tile_rows, p.tiles, stream);
 }
 
 }  // namespace mixfp4

@@ -367,6 +367,8 @@ struct ExpandArgs {
   float z;
 };
 bool adapter_expand_joins(int64_t m, int64_t n, int64_t rank, int tile_rows, int splits);
+int adapter_expand_width(const ExpandArgs& a, int tile_rows, int64_t tiles, bool dx);
+bool adapter_expand_aligned(const ExpandArgs& a, bool out16);
 hipError_t launch_adapter_expand(const ExpandArgs& a, int tile_rows, int64_t tiles, bool dx,
                                  bool out16, hipStream_t stream);
 // dA_l [rank, k] (src = x with dropout, terms of u) and dB_l [n, rank] (src =
@@ -388,6 +390,7 @@ struct GradArgs {
   int rank, padded, adapters, splits, tile_rows;
 };
 int adapter_grad_splits(int64_t m, int64_t n, int64_t k, int64_t rank);
-hipError_t launch_adapter_grad(const GradArgs& a, hipStream_t stream);
+hipError_t launch_adapter_grad(const GradArgs& q, const ExpandArgs& dx, int tile_rows, int64_t tiles,
+                               hipStream_t stream);
 
 }  // namespace mixfp4
