@@ -34,11 +34,21 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(GradArgs q) {
   for (int64_t i = ((int64_t)blockIdx.x * kSumThreads + threadIdx.x) * 4; i < matrix;
        i += (int64_t)gridDim.x * kSumThreads * 4) {
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-    for (int s = s0; s <= s1; ++s) {
-      if (piece_begin(tiles, s, q.splits) == piece_begin(tiles, s + 1, q.splits)) continue;
-      const int slot = 2 * s + (first >= piece_begin(tiles, s, q.splits));
-      v += *reinterpret_cast<const f32x4*>(a.part + slot * matrix + i);
+    // eight reads at a time; pieces without tiles hold nothing
+    for (int s = s0; s <= s1; s += 8) {
+      f32x4 u[8];
+      bool there[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int t = s + e <= s1 ? s + e : s1;
+        const int64_t begin = piece_begin(tiles, t, q.splits);
+        there[e] = s + e <= s1 && begin < piece_begin(tiles, t + 1, q.splits);
+        const int slot = there[e] ? 2 * t + (first >= begin) : 2 * s1;   // s1's is there: it enters
+        u[e] = *reinterpret_cast<const f32x4*>(a.part + slot * matrix + i);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (there[e]) v += u[e];
     }
     *reinterpret_cast<f32x4*>(a.out + l * matrix + i) = v;
   }
@@ -51,14 +61,15 @@ struct Wide {
 
 // dx and the gradients in one launch: dx is bound by memory, the gradients
 // wait for their rows and multiply, so side by side they take less than in
-// turn (8192x14336x4096 rank 64: MEASURED).  The gradients' workgroups, which
-// run long, are spread evenly over the front of the launch, up to the middle
-// of dx's.
+// turn.  The gradients' workgroups, which run long, are spread evenly over the
+// front of the launch, among the first quarter of dx's (the whole pass at
+// 8192x14336x4096 rank 64: 226 us in turn, 208 so, 225 among the first half,
+// 244 among seven eighths; 2048x11008x4096 rank 16: 65, 55.6, 58, 64).
 template <int kT, int kRank, bool kAligned>
 __global__ __launch_bounds__(kGradThreads, 2) void backward_kernel(ExpandArgs x, GradArgs q, Wide w) {
   constexpr int kDx = expand_lds(kT, kRank, true), kGrad = grad_lds(kRank);
   __shared__ uint4 lds[kDx > kGrad ? kDx : kGrad];
-  const uint64_t b = blockIdx.x, front = (uint64_t)w.grads + w.dxs / 2;
+  const uint64_t b = blockIdx.x, front = (uint64_t)w.grads + w.dxs / 4;
   if (b < front) {
     const int before = (int)(b * w.grads / front), behind = (int)((b + 1) * w.grads / front);
     if (behind > before) {
