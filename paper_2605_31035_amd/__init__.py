@@ -33,6 +33,7 @@ Functions (same names as the C ABI in include/mixfp4.h):
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import NamedTuple
 
@@ -672,7 +673,7 @@ def _probability(p) -> float:
 
 
 def _u64(v: int) -> int:
-    return int(v) & 0xFFFFFFFFFFFFFFFF
+    return operator.index(v) & 0xFFFFFFFFFFFFFFFF
 
 
 def mixfp4_dropout(x: torch.Tensor, residual: torch.Tensor | None = None, p: float = 0.5,

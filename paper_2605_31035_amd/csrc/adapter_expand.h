@@ -148,7 +148,7 @@ __device__ __forceinline__ void expand_body(const ExpandArgs& a, int width, int 
       }
       uint32_t hi[4], lo[4];
 #pragma unroll
-      for (int h = 0; h < 4; ++h) split_bf16(f * sum[h], hi[h], lo[h]);
+      for (int h = 0; h < 4; ++h) split_bf16(r + h < rank ? f * sum[h] : 0.0f, hi[h], lo[h]);
       uint2* to = reinterpret_cast<uint2*>(terms);
       to[2 * lds_slot<2 * kSlots>(q, r >> 3) + (r >> 2 & 1)] =
           make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);

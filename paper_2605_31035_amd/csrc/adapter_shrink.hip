@@ -265,15 +265,16 @@ __global__ __launch_bounds__(kThreads) void join_kernel(JoinArgs a, int tile_row
       for (int e = 1; e < kShare; ++e) sum += shared[tid + e * kItems];
     }
     if (mode == 0) sum *= a.z;
+    f32x4 scaled = s * sum;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (r + e >= rank) sum[e] = 0.0f;
+      if (r + e >= rank || row < 0) sum[e] = scaled[e] = 0.0f;   // whatever s is
     if (mode == 0 && a.t && row >= 0 && r < a.rank) {
       float* t = a.t + (int64_t)row * a.rank + r;
 #pragma unroll
       for (int e = 0; e < 4; ++e) t[e] = sum[e];
     }
-    *reinterpret_cast<f32x4*>(&v[q * kPitch + r]) = s * sum;
+    *reinterpret_cast<f32x4*>(&v[q * kPitch + r]) = scaled;
   }
   if (none) return;
   __syncthreads();

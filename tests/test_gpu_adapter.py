@@ -210,13 +210,14 @@ def test_without_c_dx_and_scaling_and_in_place():
             case.forward(0.1, out=buf[1:])
 
 
-def test_empty_batch():
+@pytest.mark.parametrize("rank", [16, 72])
+def test_empty_batch(rank):
     import paper_2605_31035_amd as M
-    case = Case(T.inputs(1, 5, 40, 64, 16, 3, False, False))
+    case = Case(T.inputs(1, 5, 40, 64, rank, 3, False, False))
     none = torch.empty(0, dtype=torch.int32, device="cuda")
     plan = M.mixfp4_adapter_plan(none, 3)
     out, t = M.mixfp4_adapter(case.x[:0], case.a, case.b, plan, keep_t=True)
-    assert out.shape == (0, 40) and t.shape == (0, 16)
+    assert out.shape == (0, 40) and t.shape == (0, rank)
     dx, da, db = M.mixfp4_adapter_backward(case.dy[:0], case.x[:0], t, case.a, case.b, plan)
     assert dx.shape == (0, 64) and not da.any() and not db.any()
 
@@ -238,6 +239,93 @@ def test_offsets_past_32_bits():
         case.forward(0.0, out=out)
     case.forward(0.0, out=c)
     assert torch.equal(c, want)
+
+
+def test_input_offsets_past_32_bits():
+    """Rows of x, dy and the gradients of x that start past 2^31 elements."""
+    d = T.inputs(9, 3, 64, 64, 8, 1, False, True)
+    d["index"][:] = 0
+    case = Case(d)
+    want, t = case.forward(0.1)
+    grads = case.backward(t, 0.1)
+    pitch = (1 << 31) + 8
+    for name in ("x", "dy"):
+        far = torch.as_strided(torch.empty(2 * pitch + 64, dtype=torch.bfloat16, device="cuda"), (3, 64),
+                               (pitch, 1))
+        far.copy_(getattr(case, name))
+        setattr(case, name, far)
+    out, t2 = case.forward(0.1)
+    assert torch.equal(out, want) and torch.equal(t2, t)
+    far = torch.as_strided(torch.empty(2 * pitch + 64, device="cuda"), (3, 64), (pitch, 1))
+    far.copy_(case.dx)
+    case.dx = far
+    for g, h in zip(case.backward(t, 0.1, out=far), grads):
+        assert torch.equal(g, h)
+
+
+@pytest.mark.parametrize("mixed", [False, True])
+def test_results_past_32_bits(mixed):
+    """2^31 results and more: the last rows against the oracle, the rows in
+    front of them against the same rows in a batch of their own."""
+    import paper_2605_31035_amd as M
+    m, n, k = 16400, 131080, 32
+    small = T.inputs(10, 40, n, k, 8, 2, mixed, False)
+    case = Case(small)
+    x = torch.randn((m, k), device="cuda").bfloat16()
+    x[-40:] = case.x
+    index = torch.zeros(m, dtype=torch.int32, device="cuda")
+    index[-40:] = _dev(small["index"])
+    plan = M.mixfp4_adapter_plan(index, 2)
+    out = torch.empty((m, n), device="cuda")
+    M.mixfp4_adapter(x, case.a, case.b, plan, out=out, **case.kw)
+    small["c"] = np.zeros_like(small["c"])
+    want, _, bound, _ = T.forward_bounds(small, 0.0, False)
+    _within("out", out[-40:], want, bound)
+    first = M.mixfp4_adapter(x[:64].contiguous(), case.a, case.b, M.mixfp4_adapter_plan(index[:64], 2),
+                             **case.kw)
+    size = first.abs().max()
+    assert (out[:64] - first).abs().max() <= 2.0**-15 * size      # other tiles, another order of sums
+
+
+@pytest.mark.parametrize("m", [20, 300])
+def test_infinite_scaling_stays_with_its_adapter(m):
+    """An infinite factor reaches its own adapter's rows and gradients, within
+    its rank."""
+    d = T.inputs(m + 1, m, 90, 136, 16, 3, False, False)
+    d["ranks"] = np.array([16, 5, 9], np.int32)
+    want, t = Case(d).forward(0.2)
+    grads = Case(d).backward(t, 0.2)
+    d["scaling"][1] = np.inf
+    case = Case(d)
+    out, t2 = case.forward(0.2)
+    own = torch.from_numpy(d["index"] == 1).cuda()
+    assert torch.equal(t2, t) and torch.equal(out[~own], want[~own]) and not torch.isfinite(out[own]).any()
+    dx, da, db = case.backward(t, 0.2)
+    assert torch.equal(dx[~own], grads[0][~own])
+    for l in (0, 2):
+        assert torch.equal(da[l], grads[1][l]) and torch.equal(db[l], grads[2][l])
+    assert not da[1, 5:].any() and not db[1, :, 5:].any()
+
+
+def test_passes_on_two_streams_at_once():
+    """Each has its own memory."""
+    cases = [Case(T.inputs(20 + i, 700, 300, 520, 32, 3, False, False)) for i in range(2)]
+    want = []
+    for c in cases:
+        out, t = c.forward(0.1)
+        want.append((out, t, *c.backward(t, 0.1)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = [[], []]
+    for _ in range(3):
+        for i, (c, s) in enumerate(zip(cases, streams)):
+            with torch.cuda.stream(s):
+                out, t = c.forward(0.1)
+                got[i].append((out, t, *c.backward(t, 0.1)))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for r in got[i]:
+            assert all(torch.equal(u, v) for u, v in zip(r, want[i]))
 
 
 def test_other_stream_and_graphs():

@@ -247,6 +247,13 @@ def test_binding_plan_and_dropout_reject():
             M.mixfp4_dropout(**{"x": x, **kw})
 
 
+def test_seeds_are_integers():
+    from paper_2605_31035_amd import _u64
+    assert _u64(-1) == 2**64 - 1 and _u64(2**64 + 3) == 3 and _u64(np.int32(5)) == 5
+    with pytest.raises(TypeError):
+        _u64(1.5)
+
+
 def test_outputs_apart_from_inputs():
     """An output is an input itself or shares nothing with it."""
     from paper_2605_31035_amd import _apart
