@@ -16,111 +16,173 @@ namespace {
 
 constexpr int kThreads = 256;
 
-template <bool kBf16>
-__device__ __forceinline__ void load_values(const void* p, int64_t at, int valid, bool wide,
-                                            float (&v)[8]) {
+// Wide accesses of any address that an element may have: rows of odd lengths
+// begin anywhere, and the memory path takes such accesses whole.
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
+// kV consecutive values of a row, 16 bytes (8 of four bf16) an access.
+template <bool kBf16, int kV>
+__device__ __forceinline__ void load_values(const void* p, int64_t at, float (&v)[kV]) {
   if constexpr (kBf16) {
     const uint16_t* q = static_cast<const uint16_t*>(p) + at;
-    if (wide) {
-      const uint4 w = *reinterpret_cast<const uint4*>(q);
-      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[2 * e] = bf16_lo(u[e]);
-        v[2 * e + 1] = bf16_hi(u[e]);
-      }
+    uint32_t w[kV == 1 ? 1 : kV / 2];
+    if constexpr (kV == 1) {
+      v[0] = __uint_as_float((uint32_t)q[0] << 16);
+      return;
+    } else if constexpr (kV == 8) {
+      const u32x4_any u = *reinterpret_cast<const u32x4_any*>(q);
+      w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
     } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = e < valid ? __uint_as_float((uint32_t)q[e] << 16) : 0.0f;
+      const u32x2_any u = *reinterpret_cast<const u32x2_any*>(q);
+      w[0] = u.x, w[1] = u.y;
     }
+#pragma unroll
+    for (int e = 0; e < kV; ++e) v[e] = e & 1 ? bf16_hi(w[e >> 1]) : bf16_lo(w[e >> 1]);
   } else {
     const float* q = static_cast<const float*>(p) + at;
-    if (wide) {
-      const float4 a = reinterpret_cast<const float4*>(q)[0];
-      const float4 b = reinterpret_cast<const float4*>(q)[1];
-      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-      v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    if constexpr (kV == 1) {
+      v[0] = q[0];
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = e < valid ? q[e] : 0.0f;
+      for (int e = 0; e < kV; e += 4) {
+        const f32x4_any a = *reinterpret_cast<const f32x4_any*>(q + e);
+        v[e] = a.x, v[e + 1] = a.y, v[e + 2] = a.z, v[e + 3] = a.w;
+      }
     }
   }
 }
 
-template <bool kBf16>
-__device__ __forceinline__ void store_values(void* p, int64_t at, int valid, bool wide,
-                                             const float (&v)[8]) {
+template <bool kBf16, int kV>
+__device__ __forceinline__ void store_values(void* p, int64_t at, const float (&v)[kV]) {
   if constexpr (kBf16) {
     uint16_t* q = static_cast<uint16_t*>(p) + at;
-    uint32_t b[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) b[e] = bf16_bits(v[e]);
-    if (wide) {
-      *reinterpret_cast<uint4*>(q) = make_uint4(b[0] | b[1] << 16, b[2] | b[3] << 16,
-                                                b[4] | b[5] << 16, b[6] | b[7] << 16);
+    if constexpr (kV == 1) {
+      q[0] = (uint16_t)bf16_bits(v[0]);
     } else {
+      uint32_t w[kV / 2];
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < valid) q[e] = (uint16_t)b[e];
+      for (int e = 0; e < kV / 2; ++e) w[e] = bf16_bits(v[2 * e]) | bf16_bits(v[2 * e + 1]) << 16;
+      if constexpr (kV == 8)
+        *reinterpret_cast<u32x4_any*>(q) = u32x4_any{w[0], w[1], w[2], w[3]};
+      else
+        *reinterpret_cast<u32x2_any*>(q) = u32x2_any{w[0], w[1]};
     }
   } else {
     float* q = static_cast<float*>(p) + at;
-    if (wide) {
-      reinterpret_cast<float4*>(q)[0] = make_float4(v[0], v[1], v[2], v[3]);
-      reinterpret_cast<float4*>(q)[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
+    if constexpr (kV == 1)
+      q[0] = v[0];
+    else
+#pragma unroll
+      for (int e = 0; e < kV; e += 4)
+        *reinterpret_cast<f32x4_any*>(q + e) = f32x4_any{v[e], v[e + 1], v[e + 2], v[e + 3]};
+  }
+}
+
+// Waves' walk over the pieces of 512 elements: `chunks` per row; a step of all
+// waves is step_rows rows and step_chunks pieces.
+struct Walk {
+  int64_t total, step_rows;
+  uint32_t chunks, step_chunks;
+};
+
+// One wave per piece of 512 elements of a row: each lane makes the draws of
+// one group of 8, then the lanes read and write side by side, kV elements
+// each, 8 / kV times, and get the keep bits of what they hold from the lane
+// that drew them.  kV is 8, or 4 if all is fp32, whose 16-byte accesses then
+// lie side by side (2^26 elements fp32 to fp32: 85 us, 6.3 TB/s, against 105;
+// with a bf16 operand 8 are better: 2^23 elements fp32 into a bf16 residual
+// 11.1 us against 13.4).  kResidual: 0 none, 1 fp32, 2 bf16.  Bound by memory:
+// 2^27 elements bf16 to bf16 90 us, 6.0 TB/s (82 without draws); rows of 8191
+// bf16 124 us, of 8191 fp32 86 us (by single elements 299 and 253).
+template <bool kX16, int kResidual, bool kOut16, int kV>
+__global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutArgs a, Walk walk) {
+  const int lane = threadIdx.x & 63;
+  // the wave's walk in scalar registers
+  const int64_t first =
+      (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t step = (int64_t)gridDim.x * (kThreads / 64);
+  int64_t row = first / walk.chunks;
+  uint32_t chunk = (uint32_t)(first - row * walk.chunks);
+  const int64_t groups = (a.k + 7) / 8;
+  for (int64_t i = first; i < walk.total; i += step) {
+    const int64_t col0 = (int64_t)chunk * 512;
+    float v[8 / kV][kV], r[8 / kV][kV];
+    const auto column = [&](int h) { return col0 + (h * 64 + lane) * kV; };
+    const bool whole = col0 + 512 <= a.k;          // else a lane looks at each of its parts
+    const int64_t xrow = row * a.ldx, rrow = row * a.ldr, orow = row * a.ldo;
+    // parts that are not there are read from the row's first element; a part
+    // that the row's end cuts is read by element
+    const auto there = [&](int h) { return whole || column(h) + kV <= a.k; };
+#pragma unroll
+    for (int h = 0; h < 8 / kV; ++h) {
+      const int64_t c = there(h) ? column(h) : 0;
+      if (whole || a.k >= kV) {
+        load_values<kX16, kV>(a.x, xrow + c, v[h]);
+        if constexpr (kResidual != 0) load_values<kResidual == 2, kV>(a.residual, rrow + c, r[h]);
+      }
+    }
+    uint32_t bits = 0xFFu;
+    if (a.drop.threshold) {
+      const uint4 w = block_draws(row * groups + (int64_t)chunk * 64 + lane, a.drop.key);
+      const uint32_t d[4] = {w.x, w.y, w.z, w.w};
+      bits = 0u;
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (e < valid) q[e] = v[e];
+        bits |= ((e & 1 ? d[e >> 1] >> 16 : d[e >> 1] & 0xFFFFu) >= a.drop.threshold ? 1u : 0u) << e;
+    }
+    const auto result = [&](float x, float res, bool keep) {
+      const float y = keep ? x * a.drop.z : 0.0f;
+      return kResidual ? res + y : y;
+    };
+#pragma unroll
+    for (int h = 0; h < 8 / kV; ++h) {
+      uint32_t mine = bits;
+      if constexpr (kV < 8) mine = __shfl(bits, (h * 64 + lane) * kV / 8) >> (lane * kV & 7);
+      if (there(h)) {
+        float y[kV];
+#pragma unroll
+        for (int e = 0; e < kV; ++e)
+          y[e] = result(v[h][e], kResidual ? r[h][e] : 0.0f, mine >> e & 1u);
+        store_values<kOut16, kV>(a.out, orow + column(h), y);
+      } else if (kV > 1 && column(h) < a.k) {
+        for (int e = 0; column(h) + e < a.k; ++e) {
+          float x[1], res[1] = {0.0f}, y[1];
+          load_values<kX16, 1>(a.x, xrow + column(h) + e, x);
+          if constexpr (kResidual != 0) load_values<kResidual == 2, 1>(a.residual, rrow + column(h) + e, res);
+          y[0] = result(x[0], res[0], mine >> e & 1u);
+          store_values<kOut16, 1>(a.out, orow + column(h) + e, y);
+        }
+      }
+    }
+    row += walk.step_rows;
+    chunk += walk.step_chunks;
+    if (chunk >= walk.chunks) {
+      chunk -= walk.chunks;
+      ++row;
     }
   }
 }
 
-// One thread per group of 8 elements.  kResidual: 0 none, 1 fp32, 2 bf16.
-template <bool kX16, int kResidual, bool kOut16>
-__global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutArgs a, uint32_t groups,
-                                                           int64_t total, bool aligned) {
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total;
-       i += (int64_t)gridDim.x * kThreads) {
-    const int64_t row = i / groups;
-    const int64_t col = (i - row * groups) * 8;
-    const int valid = a.k - col < 8 ? (int)(a.k - col) : 8;
-    const bool wide = aligned && valid == 8;
-    float v[8], r[8];
-    load_values<kX16>(a.x, row * a.ldx + col, valid, wide, v);
-    if constexpr (kResidual != 0)
-      load_values<kResidual == 2>(a.residual, row * a.ldr + col, valid, wide, r);
-    uint32_t d[4] = {0u, 0u, 0u, 0u};
-    if (a.drop.threshold) {
-      const uint4 w = block_draws(i, a.drop.key);
-      d[0] = w.x, d[1] = w.y, d[2] = w.z, d[3] = w.w;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t u = e & 1 ? d[e >> 1] >> 16 : d[e >> 1] & 0xFFFFu;
-      const float y = u >= a.drop.threshold ? v[e] * a.drop.z : 0.0f;
-      v[e] = kResidual ? r[e] + y : y;
-    }
-    store_values<kOut16>(a.out, row * a.ldo + col, valid, wide, v);
-  }
+template <bool kX16, int kResidual, bool kOut16, int kV>
+hipError_t launch_width(const DropoutArgs& a, hipStream_t stream) {
+  Walk w{};
+  w.chunks = (uint32_t)((a.k + 511) / 512);
+  w.total = a.rows * (int64_t)w.chunks;
+  static ResidentCache cache;
+  const int64_t wanted = (w.total + kThreads / 64 - 1) / (kThreads / 64);
+  const int64_t most = 16 * resident_groups(dropout_kernel<kX16, kResidual, kOut16, kV>, cache);
+  const int64_t grid = wanted < most ? wanted : most, step = grid * (kThreads / 64);
+  w.step_rows = step / w.chunks;
+  w.step_chunks = (uint32_t)(step % w.chunks);
+  dropout_kernel<kX16, kResidual, kOut16, kV><<<(unsigned)grid, kThreads, 0, stream>>>(a, w);
+  return hipGetLastError();
 }
 
 template <bool kX16, int kResidual, bool kOut16>
 hipError_t launch(const DropoutArgs& a, hipStream_t stream) {
-  const uint32_t groups = (uint32_t)((a.k + 7) / 8);
-  const int64_t total = a.rows * (int64_t)groups;
-  // 16-byte accesses: every row of every operand begins on one
-  const auto fits = [](const void* p, int64_t ld, bool half) {
-    return ((uintptr_t)p & 15) == 0 && ld % (half ? 8 : 4) == 0;
-  };
-  const bool aligned = fits(a.x, a.ldx, kX16) && fits(a.out, a.ldo, kOut16) &&
-                       (!kResidual || fits(a.residual, a.ldr, kResidual == 2));
-  static ResidentCache cache;
-  const int64_t wanted = (total + kThreads - 1) / kThreads;
-  const int64_t most = 8 * resident_groups(dropout_kernel<kX16, kResidual, kOut16>, cache);
-  dropout_kernel<kX16, kResidual, kOut16>
-      <<<(unsigned)(wanted < most ? wanted : most), kThreads, 0, stream>>>(a, groups, total, aligned);
-  return hipGetLastError();
+  return launch_width<kX16, kResidual, kOut16, !kX16 && !kOut16 && kResidual != 2 ? 4 : 8>(a, stream);
 }
 
 template <bool kX16, int kResidual>
