@@ -35,11 +35,14 @@ constexpr int expand_lds(int tile_rows, int rank, bool dx) {
 // consecutive columns, one group of dropout's draws.  The wave then turns
 // its 16 x 32 results in LDS of its own, so that 8 lanes read the base and
 // write out of one row, a whole 128-byte line (kAligned; otherwise 32 lanes,
-// 4 bytes each).  What the next block needs from memory is requested before
-// this block is stored: loads behind stores wait for them.  Loads are made
-// without branches, from a row or column that is there in place of one that
-// is not (behind the last block, from one address): with loads in a branch
-// each wait would have to assume that none are under way.  Only tiles and blocks that are not full look at each store.
+// 4 bytes each).  There the fp32 base and result pass the caches by: they are
+// used once, and W and the terms stay (8192x14336: 193 us against 202; rows
+// that do not fill lines lose by it).  What the next block needs from memory
+// is requested before this block is stored: loads behind stores wait for
+// them.  Loads are made without branches, from a row or column that is there
+// in place of one that is not (behind the last block, from one address): with
+// loads in a branch each wait would have to assume that none are under way.
+// Only tiles and blocks that are not full look at each store.
 template <int kT, int kRank, bool kDx, bool kOut16, bool kAligned, bool kJoin>
 __device__ __forceinline__ void expand_body(const ExpandArgs& a, int width, int tile, int chunk,
                                             uint4* lds) {

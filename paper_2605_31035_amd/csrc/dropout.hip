@@ -22,8 +22,22 @@ typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
+// kPass: past the caches.
+template <bool kPass, typename T>
+__device__ __forceinline__ T fetch(const void* p) {
+  if constexpr (kPass) return __builtin_nontemporal_load(static_cast<const T*>(p));
+  return *static_cast<const T*>(p);
+}
+template <bool kPass, typename T>
+__device__ __forceinline__ void put(void* p, T v) {
+  if constexpr (kPass)
+    __builtin_nontemporal_store(v, static_cast<T*>(p));
+  else
+    *static_cast<T*>(p) = v;
+}
+
 // kV consecutive values of a row, 16 bytes (8 of four bf16) an access.
-template <bool kBf16, int kV>
+template <bool kBf16, int kV, bool kPass = false>
 __device__ __forceinline__ void load_values(const void* p, int64_t at, float (&v)[kV]) {
   if constexpr (kBf16) {
     const uint16_t* q = static_cast<const uint16_t*>(p) + at;
@@ -32,10 +46,10 @@ __device__ __forceinline__ void load_values(const void* p, int64_t at, float (&v
       v[0] = __uint_as_float((uint32_t)q[0] << 16);
       return;
     } else if constexpr (kV == 8) {
-      const u32x4_any u = *reinterpret_cast<const u32x4_any*>(q);
+      const u32x4_any u = fetch<kPass, u32x4_any>(q);
       w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
     } else {
-      const u32x2_any u = *reinterpret_cast<const u32x2_any*>(q);
+      const u32x2_any u = fetch<kPass, u32x2_any>(q);
       w[0] = u.x, w[1] = u.y;
     }
 #pragma unroll
@@ -47,14 +61,14 @@ __device__ __forceinline__ void load_values(const void* p, int64_t at, float (&v
     } else {
 #pragma unroll
       for (int e = 0; e < kV; e += 4) {
-        const f32x4_any a = *reinterpret_cast<const f32x4_any*>(q + e);
+        const f32x4_any a = fetch<kPass, f32x4_any>(q + e);
         v[e] = a.x, v[e + 1] = a.y, v[e + 2] = a.z, v[e + 3] = a.w;
       }
     }
   }
 }
 
-template <bool kBf16, int kV>
+template <bool kBf16, int kV, bool kPass = false>
 __device__ __forceinline__ void store_values(void* p, int64_t at, const float (&v)[kV]) {
   if constexpr (kBf16) {
     uint16_t* q = static_cast<uint16_t*>(p) + at;
@@ -65,9 +79,9 @@ __device__ __forceinline__ void store_values(void* p, int64_t at, const float (&
 #pragma unroll
       for (int e = 0; e < kV / 2; ++e) w[e] = bf16_bits(v[2 * e]) | bf16_bits(v[2 * e + 1]) << 16;
       if constexpr (kV == 8)
-        *reinterpret_cast<u32x4_any*>(q) = u32x4_any{w[0], w[1], w[2], w[3]};
+        put<kPass>(q, u32x4_any{w[0], w[1], w[2], w[3]});
       else
-        *reinterpret_cast<u32x2_any*>(q) = u32x2_any{w[0], w[1]};
+        put<kPass>(q, u32x2_any{w[0], w[1]});
     }
   } else {
     float* q = static_cast<float*>(p) + at;
@@ -76,7 +90,7 @@ __device__ __forceinline__ void store_values(void* p, int64_t at, const float (&
     else
 #pragma unroll
       for (int e = 0; e < kV; e += 4)
-        *reinterpret_cast<f32x4_any*>(q + e) = f32x4_any{v[e], v[e + 1], v[e + 2], v[e + 3]};
+        put<kPass>(q + e, f32x4_any{v[e], v[e + 1], v[e + 2], v[e + 3]});
   }
 }
 
@@ -93,10 +107,12 @@ struct Walk {
 // that drew them.  kV is 8, or 4 if all is fp32, whose 16-byte accesses then
 // lie side by side (2^26 elements fp32 to fp32: 85 us, 6.3 TB/s, against 105;
 // with a bf16 operand 8 are better: 2^23 elements fp32 into a bf16 residual
-// 11.1 us against 13.4).  kResidual: 0 none, 1 fp32, 2 bf16.  Bound by memory:
-// 2^27 elements bf16 to bf16 90 us, 6.0 TB/s (82 without draws); rows of 8191
-// bf16 124 us, of 8191 fp32 86 us (by single elements 299 and 253).
-template <bool kX16, int kResidual, bool kOut16, int kV>
+// 11.5 us against 13.4).  kResidual: 0 none, 1 fp32, 2 bf16.  Bound by memory:
+// 2^27 elements bf16 to bf16 87 us, 6.2 TB/s (92 through the caches, where
+// what fits into the infinity cache is better off: 11.5 against 12.3 us for
+// 2^23 elements); rows of 8191 bf16 124 us, of 8191 fp32 87 us (by single
+// elements 299 and 253).
+template <bool kX16, int kResidual, bool kOut16, int kV, bool kPass>
 __global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutArgs a, Walk walk) {
   const int lane = threadIdx.x & 63;
   // the wave's walk in scalar registers
@@ -119,8 +135,8 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutArgs a, Walk w
     for (int h = 0; h < 8 / kV; ++h) {
       const int64_t c = there(h) ? column(h) : 0;
       if (whole || a.k >= kV) {
-        load_values<kX16, kV>(a.x, xrow + c, v[h]);
-        if constexpr (kResidual != 0) load_values<kResidual == 2, kV>(a.residual, rrow + c, r[h]);
+        load_values<kX16, kV, kPass>(a.x, xrow + c, v[h]);
+        if constexpr (kResidual != 0) load_values<kResidual == 2, kV, kPass>(a.residual, rrow + c, r[h]);
       }
     }
     uint32_t bits = 0xFFu;
@@ -145,7 +161,7 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutArgs a, Walk w
 #pragma unroll
         for (int e = 0; e < kV; ++e)
           y[e] = result(v[h][e], kResidual ? r[h][e] : 0.0f, mine >> e & 1u);
-        store_values<kOut16, kV>(a.out, orow + column(h), y);
+        store_values<kOut16, kV, kPass>(a.out, orow + column(h), y);
       } else if (kV > 1 && column(h) < a.k) {
         for (int e = 0; column(h) + e < a.k; ++e) {
           float x[1], res[1] = {0.0f}, y[1];
@@ -165,24 +181,36 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutArgs a, Walk w
   }
 }
 
-template <bool kX16, int kResidual, bool kOut16, int kV>
+template <bool kX16, int kResidual, bool kOut16, int kV, bool kPass>
 hipError_t launch_width(const DropoutArgs& a, hipStream_t stream) {
   Walk w{};
   w.chunks = (uint32_t)((a.k + 511) / 512);
   w.total = a.rows * (int64_t)w.chunks;
   static ResidentCache cache;
   const int64_t wanted = (w.total + kThreads / 64 - 1) / (kThreads / 64);
-  const int64_t most = 16 * resident_groups(dropout_kernel<kX16, kResidual, kOut16, kV>, cache);
+  const int64_t most = 16 * resident_groups(dropout_kernel<kX16, kResidual, kOut16, kV, kPass>, cache);
   const int64_t grid = wanted < most ? wanted : most, step = grid * (kThreads / 64);
   w.step_rows = step / w.chunks;
   w.step_chunks = (uint32_t)(step % w.chunks);
-  dropout_kernel<kX16, kResidual, kOut16, kV><<<(unsigned)grid, kThreads, 0, stream>>>(a, w);
+  dropout_kernel<kX16, kResidual, kOut16, kV, kPass><<<(unsigned)grid, kThreads, 0, stream>>>(a, w);
   return hipGetLastError();
 }
 
 template <bool kX16, int kResidual, bool kOut16>
 hipError_t launch(const DropoutArgs& a, hipStream_t stream) {
-  return launch_width<kX16, kResidual, kOut16, !kX16 && !kOut16 && kResidual != 2 ? 4 : 8>(a, stream);
+  constexpr int kV = !kX16 && !kOut16 && kResidual != 2 ? 4 : 8;
+  constexpr int kBytes[3] = {0, 4, 2};
+  const int64_t bytes = a.rows * a.k * ((kX16 ? 2 : 4) + kBytes[kResidual] + (kOut16 ? 2 : 4));
+  // past the caches where the operands do not fit into the infinity cache
+  // (256 MB) and rows fill whole accesses
+  const auto fits = [](const void* p, int64_t ld, bool half) {
+    const int64_t size = half ? 2 : 4;
+    return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0;
+  };
+  if (bytes > (int64_t(256) << 20) && fits(a.x, a.ldx, kX16) && fits(a.out, a.ldo, kOut16) &&
+      (!kResidual || fits(a.residual, a.ldr, kResidual == 2)))
+    return launch_width<kX16, kResidual, kOut16, kV, true>(a, stream);
+  return launch_width<kX16, kResidual, kOut16, kV, false>(a, stream);
 }
 
 template <bool kX16, int kResidual>

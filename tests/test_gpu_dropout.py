@@ -101,6 +101,26 @@ def test_rows_past_32_bits():
     assert not y[:-2].any()
 
 
+@pytest.mark.parametrize("xt,rt,ot", [(F32, None, F32), (F32, BF16, BF16), (BF16, F32, F32),
+                                      (BF16, BF16, BF16)])
+@pytest.mark.parametrize("k", [16384, 16392, 16385])
+def test_larger_than_the_infinity_cache(xt, rt, ot, k):
+    """More than 256 MB of operands, in rows of whole accesses and not: the
+    first and last rows against the oracle."""
+    import paper_2605_31035_amd as M
+    rows = (300 << 20) // (k * (xt.itemsize + (rt.itemsize if rt else 0) + ot.itemsize)) + 1
+    x, r = (None if t is None else torch.randn((rows, k), device="cuda").to(t) for t in (xt, rt))
+    y = M.mixfp4_dropout(x, residual=r, p=0.2, seed=SEED, offset=OFFSET, out_dtype=ot)
+    for at in (0, rows - 3):
+        f = AD.factors(3, k, 0.2, SEED, OFFSET, row_index=np.arange(at, at + 3))
+        scaled = _f64(x[at:at + 3]) * f
+        want = scaled + (0.0 if r is None else _f64(r[at:at + 3]))
+        bound = 2.0**-23 * abs(scaled) + 2.0**-24 * abs(want) + 2.0**-40 * (abs(scaled) + abs(want))
+        if ot == BF16:
+            bound = bound + 2.0**-8 * (abs(want) + bound)
+        assert (abs(_f64(y[at:at + 3]) - want) <= bound).all()
+
+
 def test_gradient_is_the_same_call():
     import paper_2605_31035_amd as M
     x, dy = _make(5, (64, 136), F32), _make(6, (64, 136), F32)
