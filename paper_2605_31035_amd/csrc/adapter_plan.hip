@@ -77,10 +77,14 @@ __global__ __launch_bounds__(kThreads) void adapter_plan_kernel(const int32_t* i
 
 }  // namespace
 
-// Rows of a tile: 16 where few rows meet an adapter (their time is the read
-// of the adapters), 64 where the rows are many.
+// Rows of a tile: 16 where few rows meet an adapter, whose tiles of 64 would
+// be mostly empty and too few to fill the device, and 64 where W is read less
+// often so.  Forward and backward pass of a 4096 x 4096 layer, us, with 16 and
+// with 64 rows: 255 rows of one adapter 17.8 and 19.8, 31.5 and 32.0; 512 rows
+// 20.2 and 21.2, 35.9 and 36.6; 1024 rows of 32 adapters (rank 64) 28.8 and
+// 32.4, 98 and 104; 4096 of 128 (rank 16) 49 and 53, 152 and 145.
 int adapter_tile_rows(int64_t rows, int64_t adapters) {
-  return rows < 256 || rows < 24 * adapters ? 16 : 64;
+  return rows <= 512 || rows <= 32 * adapters ? 16 : 64;
 }
 
 // ceil(c / T) summed over the groups is at most rows / T + groups, and at

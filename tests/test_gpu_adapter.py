@@ -71,7 +71,9 @@ SHAPES = [(1, 1, 8, 8, 1, False, True), (1, 64, 64, 16, 3, False, True), (2, 130
           (333, 1000, 384, 8, 3, True, True), (300, 257, 520, 72, 7, False, False),
           (509, 264, 2056, 32, 6, True, True), (700, 135, 1288, 136, 2, False, True),
           (1030, 300, 1032, 256, 2, False, True), (2049, 96, 264, 64, 40, True, False),
-          (2048, 1100, 256, 128, 1, False, True), (4500, 72, 136, 16, 200, True, False)]
+          (2048, 1100, 256, 128, 1, False, True), (4500, 72, 136, 16, 200, True, False),
+          (513, 1000, 384, 8, 3, True, True), (768, 129, 264, 16, 1, False, True),
+          (640, 200, 512, 32, 3, True, False), (1200, 257, 520, 64, 7, True, False)]
 
 
 @pytest.mark.parametrize("p", [0.0, 0.3])
@@ -96,7 +98,7 @@ def test_forward_and_backward(shape, p):
         assert torch.equal(g, h)
 
 
-@pytest.mark.parametrize("m", [3, 70, 600])
+@pytest.mark.parametrize("m", [3, 70, 600, 1500])
 def test_no_row_has_an_adapter(m):
     d = T.inputs(m, m, 96, 64, 16, 3, False, False)
     d["index"][:] = np.where(np.arange(m) % 2, -1, 3)
@@ -107,7 +109,7 @@ def test_no_row_has_an_adapter(m):
     assert torch.equal(dx, case.dx) and not da.any() and not db.any()
 
 
-@pytest.mark.parametrize("m", [24, 300])
+@pytest.mark.parametrize("m", [24, 300, 700])
 def test_rank_zero_and_p_one(m):
     d = T.inputs(m, m, 96, 64, 16, 2, False, False)
     d["ranks"] = np.array([0, -5], np.int32)
@@ -124,7 +126,7 @@ def test_rank_zero_and_p_one(m):
     assert torch.equal(dx, case.dx) and not da.any() and not db.any()
 
 
-@pytest.mark.parametrize("m,rank", [(20, 16), (40, 72), (400, 16), (700, 136)])
+@pytest.mark.parametrize("m,rank", [(20, 16), (40, 72), (400, 16), (600, 16), (700, 136), (900, 64)])
 def test_unread_places_hold_anything(m, rank):
     """NaN in dropped elements of x, in rows without an adapter, behind an
     adapter's rank, in adapters that no row has: nothing changes."""
@@ -159,7 +161,7 @@ def test_unread_places_hold_anything(m, rank):
         assert torch.equal(g, h)
 
 
-@pytest.mark.parametrize("m", [24, 300])
+@pytest.mark.parametrize("m", [24, 300, 700])
 def test_infinite_values_stay_where_they_belong(m):
     d = T.inputs(m, m, 96, 64, 16, 2, False, False)
     d["index"][:] = np.arange(m) % 2
@@ -179,7 +181,7 @@ def test_infinite_values_stay_where_they_belong(m):
 
 def test_without_c_dx_and_scaling_and_in_place():
     import paper_2605_31035_amd as M
-    for m in (9, 300):
+    for m in (9, 300, 600):
         d = T.inputs(m, m, 96, 64, 16, 2, False, False)
         d["scaling"][:] = 1.0
         case = Case(d)
@@ -287,7 +289,7 @@ def test_results_past_32_bits(mixed):
     assert (out[:64] - first).abs().max() <= 2.0**-15 * size      # other tiles, another order of sums
 
 
-@pytest.mark.parametrize("m", [20, 300])
+@pytest.mark.parametrize("m", [20, 300, 700])
 def test_infinite_scaling_stays_with_its_adapter(m):
     """An infinite factor reaches its own adapter's rows and gradients, within
     its rank."""
@@ -332,7 +334,7 @@ def test_other_stream_and_graphs():
     """A call on another stream, and two captured passes that are replayed
     between eager ones on the same inputs."""
     import paper_2605_31035_amd as M
-    for m in (12, 400):
+    for m in (12, 400, 800):
         case = Case(T.inputs(m, m, 200, 264, 16, 3, True, False))
         index = _dev(case.d["index"])
         out, t = case.forward(0.2)
