@@ -60,7 +60,7 @@ int adapter_expand_width(const ExpandArgs& a, int tile_rows, int64_t tiles, bool
   // the device stays full.  A rank above 128 leaves room for one workgroup per
   // compute unit: as many as there are units (1537x4096 rank 256: 55 us with
   // one block each, 46 with four, 49 with five).  Else two (8192x14336 rank 64:
-  // 200 us with one, 191 with two, 204 with three), one below 3072 workgroups
+  // 200 us with one, 191 with two, 204 with three), one below 6000 workgroups
   // (2048x11008: the same with one to three); the input gradient pays more for
   // a workgroup's start (8192x4096: 62 us with one, 56 with two).  Tiles of 16
   // rows: 1024 workgroups (48x11008 rank 64: 22 us with one, 19 with three).
@@ -72,7 +72,7 @@ int adapter_expand_width(const ExpandArgs& a, int tile_rows, int64_t tiles, bool
   else if (padded_rank(a.rank) > 128)
     w = (units + compute_units() - 1) / compute_units();
   else
-    w = (dx ? units + 3071 : units) / 3072 < 2 ? 1 : 2;
+    w = units >= (dx ? 3000 : 6000) ? 2 : 1;
   if (w > 8) w = 8;
   return 128 * (w < 1 ? 1 : (int)w);
 }
