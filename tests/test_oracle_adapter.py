@@ -122,6 +122,7 @@ def test_adapter_rejects(lib):
                                   0, 0, t, out, ot, ldo, ws, wb, None)
     for kw in SHAPES + [dict(p=2.0), dict(ldx=60), dict(ldx=68), dict(ldc=47), dict(ldo=47), dict(wb=0)]:
         assert f(**kw) == 2, kw
+    assert f(ldc=1 << 32) == 2 and f(ldo=1 << 32) == 2 and f(ldx=1 << 32) == 2
     assert f(ot=2) == 4
     for name in ("x", "a", "b", "plan", "out", "ws"):
         assert f(**{name: None}) == 1, name
