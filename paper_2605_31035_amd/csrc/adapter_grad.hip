@@ -105,7 +105,8 @@ int64_t blocks_of(int64_t cols, int64_t rank) {
 // two workgroups per compute unit at best, and write and read more partial
 // sums: 8 bytes an element of the gradients against 2 an element of x and dy.
 int adapter_grad_splits(int64_t m, int64_t n, int64_t k, int64_t rank) {
-  const int64_t blocks = (blocks_of(n, rank) + blocks_of(k, rank)) * (rank > 128 ? 2 : 1), round = 2 * compute_units();
+  const int64_t blocks = (blocks_of(n, rank) + blocks_of(k, rank)) * (rank > 128 ? 2 : 1);
+  const int64_t round = 2 * compute_units();
   int best = 1;
   double score = 0.0;
   for (int64_t s = 1; s <= 64 && (s == 1 || s * 64 <= m); ++s) {
