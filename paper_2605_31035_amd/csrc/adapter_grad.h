@@ -58,7 +58,9 @@ __device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, 
 
   f32x4 acc[kTiles][kSide];
   const int wave_col = wave * 16 * kSide;
-  const auto store = [&](float* to) {
+  // Behind the adapter's own rank stand zeros: the terms are zero there, but
+  // zero times an infinite x or dy is not.
+  const auto store = [&](float* to, int own) {
     // opaque, so that the addresses are made here and not kept in registers
     // over the steps
     int r16 = lane & 15, g = lane >> 4;
@@ -70,7 +72,10 @@ __device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, 
 #pragma unroll
         for (int j = 0; j < kSide; ++j) {
           const int n = col0 + wave_col + 16 * j + r16;
-          if (n < a.cols && r < q.rank) *reinterpret_cast<f32x4*>(to + (int64_t)n * q.rank + r) = acc[i][j];
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = r + e < own ? acc[i][j][e] : 0.0f;
+          if (n < a.cols && r < q.rank) *reinterpret_cast<f32x4*>(to + (int64_t)n * q.rank + r) = v;
         }
       } else {
         const int r = r0 + 16 * i + r16;
@@ -78,7 +83,8 @@ __device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, 
         for (int j = 0; j < kSide; ++j) {
           const int c = col0 + wave_col + 32 * (j >> 1) + 8 * g;
           if (r < q.rank && c < a.cols)
-            *reinterpret_cast<f32x4*>(to + (int64_t)r * a.cols + c + 4 * (j & 1)) = acc[i][j];
+            *reinterpret_cast<f32x4*>(to + (int64_t)r * a.cols + c + 4 * (j & 1)) =
+                r < own ? acc[i][j] : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
       }
     }
@@ -94,7 +100,7 @@ __device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, 
     for (int l = 0; l < q.adapters; ++l)
       if (q.plan.seg[l] == q.plan.seg[l + 1]) {
         clear();
-        store(a.out + l * matrix);
+        store(a.out + l * matrix, 0);
       }
   if (t0 >= t1) return;
 
@@ -211,10 +217,11 @@ __device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, 
           }
       }
     }
+    const int own = rank_of(q.ranks, l, q.rank);
     if (first >= t0 && last <= t1)
-      store(a.out + l * matrix);
+      store(a.out + l * matrix, own);
     else
-      store(a.part + (2 * piece + (first >= t0)) * matrix);
+      store(a.part + (2 * piece + (first >= t0)) * matrix, own);
   }
 }
 

@@ -89,7 +89,7 @@ hipError_t launch_adapter_backward(const AdapterArgs& a, hipStream_t stream) {
   const int rank = (int)a.rank, adapters = (int)a.adapters;
   const GradArgs grad{{a.x, a.ldx, p.terms_t, p.part_a, a.da, (int)a.k},
                       {a.dy, a.lddy, p.t_t, p.part_b, a.db, (int)a.n},
-                      a.plan, a.drop, p.positions, rank, p.padded, adapters, p.grad_splits, p.tile_rows};
+                      a.ranks, a.plan, a.drop, p.positions, rank, p.padded, adapters, p.grad_splits, p.tile_rows};
   ExpandArgs x{};
   x.terms = p.terms, x.w = a.a, x.ranks = a.ranks, x.plan = a.plan, x.drop = a.drop;
   x.base = a.dx0, x.ldb = a.lddx0, x.out = a.dx, x.ldo = a.lddx;

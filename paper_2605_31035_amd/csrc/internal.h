@@ -384,6 +384,7 @@ struct GradSide {
 };
 struct GradArgs {
   GradSide a, b;
+  const int32_t* ranks;
   AdapterPlan plan;
   DropParams drop;
   int64_t positions;
