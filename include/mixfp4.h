@@ -512,10 +512,11 @@ int mixfp4_dropout(const void *x, int32_t x_type, int64_t ldx,
  *   u_i  = s_l dy_i B_l                    dx_i  = dx_in_i + z keep_i (u_i A_l)
  *   dA_l = z sum_i u_i^T (keep_i x_i)      dB_l  = s_l sum_i dy_i^T t_i
  * Rows without an adapter get out = c, t = 0 and dx = dx_in; adapters without
- * rows get gradients of zero.  Row pitches are below 2^32.  Sums are fp32; t and u enter the products
- * behind them as bf16 terms, two for out and dx (relative error 2^-17), three
- * for dA and dB.  Results are deterministic.  Infinities and NaN are taken; they stay within what depends
- * on them.
+ * rows get gradients of zero.  Row pitches are below 2^32.  Sums are fp32; t
+ * and u enter the products behind them as bf16 terms, two for out and dx
+ * (relative error 2^-17), three, which hold all their bits, for dA and dB.
+ * Results are deterministic.  Infinities and NaN are taken: what depends on
+ * them has the values that these formulas give it, and nothing else changes.
  *
  * mixfp4_adapter_plan - the rows grouped by adapter, for any number of calls
  * on the same rows (every projection of a batch).

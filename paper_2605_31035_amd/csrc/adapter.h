@@ -11,8 +11,7 @@
 // bf16 terms.  Two terms in the products that a matrix is added to (out, dx):
 // |t - hi - lo| <= 2^-17 |t| (2^e <= |t|: a step of hi is 2^(e-7), the rest at
 // most 2^(e-8) and its own step below that 2^(e-16)), about 2^-19 in the mean.
-// Three in dA and dB, which stand alone: the rest of two is at most 2^(e-17),
-// so the third leaves 2^-26 |t|, less than t's own rounding.  With two the
+// Three in dA and dB, which stand alone: they hold t's 24 bits.  With two the
 // gradients were 2.5e-6 from the exact ones, where fp32 operands give 3e-7
 // (333 rows) to 2e-6 (8192 rows).
 //
@@ -47,11 +46,22 @@ __device__ __forceinline__ void split_bf16(float v, uint32_t& hi, uint32_t& lo) 
   lo = (hi & 0x7F80u) == 0x7F80u ? 0u : bf16_bits(v - h);
 }
 
-// v = hi + mid + lo.
-__device__ __forceinline__ void split_bf16(float v, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
-  split_bf16(v, hi, mid);
-  const float rest = (v - __uint_as_float(hi << 16)) - __uint_as_float(mid << 16);
-  lo = (hi & 0x7F80u) == 0x7F80u ? 0u : bf16_bits(rest);
+// v = a[0] + a[1] + a[2], exactly, none of them zero unless v is and all of
+// v's sign: an infinite operand's products with them are infinite where its
+// product with v is.  v's 24 bits give up to three terms of eight; where there
+// are fewer, the first is taken in parts.  An infinity or NaN stands in all
+// three.  (Below 2^-109 the last step of bf16, 2^-133, bounds it.)
+__device__ __forceinline__ void split_bf16(float v, uint32_t (&a)[3]) {
+  const float first = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u), rest = v - first;
+  const float second = __uint_as_float(__float_as_uint(rest) & 0xFFFF0000u), third = rest - second;
+  float t[3] = {first, second, third};
+  if (third == 0.0f) {
+    t[0] = 0.5f * first;
+    t[1] = second == 0.0f ? 0.25f * first : 0.5f * first;
+    t[2] = second == 0.0f ? 0.25f * first : second;
+  }
+#pragma unroll
+  for (int e = 0; e < 3; ++e) a[e] = bf16_bits(fabsf(v) < __builtin_huge_valf() ? t[e] : v);
 }
 
 // The keep bits of 8 consecutive elements from their group's draws: element e

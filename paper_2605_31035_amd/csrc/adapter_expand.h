@@ -261,6 +261,32 @@ __device__ __forceinline__ void expand_body(const ExpandArgs& a, int width, int 
           }
         }
       }
+      // An infinite W times a second term of zero, or of the other sign than
+      // the first, is NaN where the product is infinite: what is NaN is made
+      // again of the first terms, whose products have the infinities and NaN of
+      // the whole.
+      bool lost = false;
+#pragma unroll
+      for (int e = 0; e < 8 * kRows; ++e) {
+        const float v = acc[e >> 3][e >> 2 & 1][e & 3];
+        lost |= v != v;
+      }
+      if (__builtin_expect(__any(lost), 0)) {
+        int r = r16, k = g;        // opaque, so that the addresses are made here
+        asm volatile("" : "+v"(r), "+v"(k));
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            f32x4 first = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+            for (int s = 0; s * 32 < rank; ++s)
+              first = mfma16(wt[lds_slot<kSlots>(wave_col + 8 * (r >> 2) + 4 * j + (r & 3), 4 * s + k)],
+                             terms[lds_slot<2 * kSlots>(row0 + i * 16 + r, 4 * s + k)], first);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = acc[i][j][e] == acc[i][j][e] ? acc[i][j][e] : first[e];
+          }
+      }
       if (!kAhead) load_w(block + 128, more);
 #pragma unroll
       for (int i = 0; i < kRows; ++i) {

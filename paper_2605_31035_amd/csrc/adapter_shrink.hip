@@ -300,8 +300,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(JoinArgs a, int tile_row
     for (int i = tid; i < 8 * kRank; i += kThreads) {
       const int q = i % 8 * 2, r = i / 8;
       uint32_t x[3], y[3];
-      split_bf16(v[q * kPitch + r], x[0], x[1], x[2]);
-      split_bf16(v[(q + 1) * kPitch + r], y[0], y[1], y[2]);
+      split_bf16(v[q * kPitch + r], x);
+      split_bf16(v[(q + 1) * kPitch + r], y);
 #pragma unroll
       for (int h = 0; h < 3; ++h)
         *reinterpret_cast<uint32_t*>(transposed + ((int64_t)h * kRank + r) * a.positions + p0 + q) =

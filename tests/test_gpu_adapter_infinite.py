@@ -52,3 +52,83 @@ def test_gradients_behind_a_rank_are_zero(m, rank):
             # what holds them reaches its adapter
             hit = da if name == "x" else db
             assert not torch.isfinite(hit[2, :5] if name == "x" else hit[2, :, :5]).all()
+
+
+def _same(name, got, want, clean):
+    """The definition's infinities and NaN, and every finite value as without
+    them (it does not depend on them), bit for bit."""
+    got = host(got)
+    inf, nan = np.isinf(want), np.isnan(want)
+    assert inf.any()
+    assert (got[inf] == want[inf]).all(), f"{name}: {(got[inf] != want[inf]).sum()} of {inf.sum()} infinities"
+    assert np.isnan(got[nan]).all(), name
+    rest = ~(inf | nan)
+    assert (got[rest] == host(clean)[rest]).all(), name
+
+
+@pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("m,rank", SIZES)
+def test_infinite_operands_forward(m, rank, out_dtype):
+    """t enters the wide product in two terms, the second of either sign or
+    zero: an infinite element of B times t is infinite all the same, and so is
+    one of x behind a rank of one."""
+    log(f"infinite forward {m} {rank} {out_dtype}")
+    d = _inputs(m, rank)
+    d["ranks"][1] = 1
+    d["x"][3] = 0.0
+    d["x"][3, 0] = 1.0                       # t of row 3 has an element of one term, 1.0
+    d["a"][0, 2, 0] = 1.0
+    for pitch in (0, 1):
+        clean, t = Case(d, pitch).forward(0.0, out_dtype)
+        e = dict(d, x=d["x"].copy(), b=d["b"].copy())
+        e["x"][4, 11] = np.inf               # adapter 1: t is one infinity
+        e["b"][0, 7, 2], e["b"][0, 88, 5], e["b"][1, 8, 0], e["b"][2, 0, 4] = np.inf, -np.inf, np.inf, -np.inf
+        e["b"][2, 89, 1], e["b"][2, 89, 3] = np.inf, np.nan
+        out, t2 = Case(e, pitch).forward(0.0, out_dtype)
+        with np.errstate(invalid="ignore"):
+            want, wt = AD.forward(e["x"], e["a"], e["b"], e["index"], c=e["c"], scaling=e["scaling"],
+                                  ranks=e["ranks"])
+        _same("out", out, want, clean) if out_dtype == torch.float32 else \
+            _same("out", out.float(), want, clean.float())
+        _same("t", t2, wt, t)
+        assert out[3, 7] == np.inf
+
+
+@pytest.mark.parametrize("p", [0.0, 0.3])
+@pytest.mark.parametrize("m,rank", SIZES)
+def test_infinite_operands_backward(m, rank, p):
+    """t and u enter the gradients' products in three terms and dx in two: an
+    infinite element of x, dy or A times them is infinite all the same."""
+    log(f"infinite backward {m} {rank} p={p}")
+    d = _inputs(m, rank)
+    d["ranks"][1] = 1
+    for pitch in (0, 1):
+        case = Case(d, pitch)
+        _, t = case.forward(p)
+        t[3, 0] = 1.0                        # a row of terms (1, 0, 0)
+        clean = case.backward(t, p)
+        kept = AD.factors(m, 136, p, SEED, OFFSET) != 0
+        for name in ("x", "dy", "a"):
+            e = dict(d, **{name: d[name].copy()})
+            if name == "a":
+                e["a"][0, 3, 5], e["a"][0, 0, 135], e["a"][1, 0, 64], e["a"][2, 4, 0] = np.inf, -np.inf, np.inf, np.nan
+            else:
+                for i, value in ((3, np.inf), (4, -np.inf), (5, np.inf), (m - 1, -np.inf), (m - 2, np.nan)):
+                    e[name][i, np.flatnonzero(kept[i, :90])[i % 7]] = value
+            with np.errstate(invalid="ignore"):
+                want = AD.backward(e["dy"], e["x"], host(t), e["a"], e["b"], e["index"], dx=e["dx"],
+                                   scaling=e["scaling"], ranks=e["ranks"], p=p, seed=SEED, offset=OFFSET)
+            got = Case(e, pitch).backward(t, p)
+            hits = dict(x=(1,), dy=(0, 1, 2), a=(0,))[name]
+            for i, part in enumerate(("dx", "da", "db")):
+                if i not in hits:
+                    assert torch.equal(got[i], clean[i]), (name, part)
+                elif name == "dy" and i < 2:
+                    # u of such a row is infinite: what stands beside it is not the clean value's bits,
+                    # but the rows and adapters without one are
+                    inf, nan = np.isinf(want[i]), np.isnan(want[i])
+                    g = host(got[i])
+                    assert (g[inf] == want[i][inf]).all() and np.isnan(g[nan]).all(), (name, part)
+                    assert np.isfinite(g[~(inf | nan)]).all(), (name, part)
+                else:
+                    _same(f"{part} of {name}", got[i], want[i], clean[i])
