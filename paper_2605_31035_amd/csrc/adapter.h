@@ -10,7 +10,8 @@
 // and exact there.  t and u are fp32 sums; as operands they are carried as
 // bf16 terms.  Two terms in the products that a matrix is added to (out, dx):
 // |t - hi - lo| <= 2^-17 |t| (2^e <= |t|: a step of hi is 2^(e-7), the rest at
-// most 2^(e-8) and its own step below that 2^(e-16)), about 2^-19 in the mean.
+// most 2^(e-8) and its own step below that 2^(e-16); 2^-16.9 where t is above
+// the largest bf16), about 2^-19 in the mean.
 // Three in dA and dB, which stand alone: they hold t's 24 bits.  With two the
 // gradients were 2.5e-6 from the exact ones, where fp32 operands give 3e-7
 // (333 rows) to 2e-6 (8192 rows).
@@ -39,11 +40,14 @@ __device__ __forceinline__ uint32_t bf16_bits(float v) {
   return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
-// v = hi + lo in bf16; an infinity or NaN stays whole in hi.
+// v = hi + lo in bf16; an infinity or NaN stays whole in hi.  A finite v above
+// the largest bf16, which rounds to infinity, takes that one.
 __device__ __forceinline__ void split_bf16(float v, uint32_t& hi, uint32_t& lo) {
+  const bool finite = fabsf(v) < __builtin_huge_valf();
   hi = bf16_bits(v);
+  if (finite && (hi & 0x7F80u) == 0x7F80u) --hi;
   const float h = __uint_as_float(hi << 16);
-  lo = (hi & 0x7F80u) == 0x7F80u ? 0u : bf16_bits(v - h);
+  lo = finite ? bf16_bits(v - h) : 0u;
 }
 
 // v = a[0] + a[1] + a[2], exactly, none of them zero unless v is and all of

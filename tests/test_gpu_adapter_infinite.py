@@ -132,3 +132,49 @@ def test_infinite_operands_backward(m, rank, p):
                     assert np.isfinite(g[~(inf | nan)]).all(), (name, part)
                 else:
                     _same(f"{part} of {name}", got[i], want[i], clean[i])
+
+
+@pytest.mark.parametrize("m,rank", [(24, 16), (24, 72), (600, 24), (600, 200)])
+def test_largest_finite_terms(m, rank):
+    """t and u between the largest bf16 (255/128 2^127) and the largest fp32:
+    their products with small operands are finite, within 2^-17 for the terms
+    (2^-16.9 at this end) and a few fp32 steps (2^-21)."""
+    import paper_2605_31035_amd as M
+    bf = torch.bfloat16
+    top, small, tiny = 255 / 128 * 2.0**63, 2.0**56, 2.0**-100
+    t_value = 65535 / 32768 * 2.0**127       # (2^64 + 2^56) 255/128 2^63, exact in fp32
+    bound = 2.0**-16.9 + 2.0**-21
+    plan = M.mixfp4_adapter_plan(torch.zeros(m, dtype=torch.int32, device="cuda"), 1)
+
+    def full(shape, value):
+        return torch.full(shape, value, dtype=bf, device="cuda")
+
+    sign = torch.ones((m, 1), device="cuda", dtype=bf)
+    sign[::2] = -1
+    # t = +-t_value in its first element, zero behind it
+    x = torch.zeros((m, 64), dtype=bf, device="cuda")
+    x[:, :2] = sign * top
+    a = torch.zeros((1, rank, 64), dtype=bf, device="cuda")
+    a[0, 0, 0], a[0, 0, 1] = 2.0**64, small
+    out, t = M.mixfp4_adapter(x, a, full((1, 40, rank), tiny), plan, keep_t=True)
+    s = host(sign.double())
+    assert (host(t[:, 0].double()) == s[:, 0] * t_value).all() and not t[:, 1:].any()
+    want = s * t_value * tiny
+    assert (abs(host(out.double()) - want) <= bound * abs(want)).all()
+    # dB from such a t: the sum over the rows, all of one sign
+    _, _, db = M.mixfp4_adapter_backward(sign.expand(m, 40).contiguous() * tiny, x, t, a,
+                                         full((1, 40, rank), tiny), plan)
+    want = m * t_value * tiny
+    sums = (m + 8) * 2.0**-23
+    assert (abs(host(db[0, :, 0].double()) - want) <= (bound + 3 * sums) * want).all()
+    assert not db[0, :, 1:].any()
+    # u = +-t_value: dx and dA
+    dy = torch.zeros((m, 40), dtype=bf, device="cuda")
+    dy[:, :2] = sign * top
+    b = torch.zeros((1, 40, rank), dtype=bf, device="cuda")
+    b[0, 0, 0], b[0, 1, 0] = 2.0**64, small
+    dx, da, _ = M.mixfp4_adapter_backward(dy, sign.expand(m, 64).contiguous() * tiny, torch.zeros_like(t),
+                                          full((1, rank, 64), tiny), b, plan)
+    assert (abs(host(dx.double()) - s * t_value * tiny) <= bound * t_value * tiny).all()
+    assert (abs(host(da[0, 0].double()) - want) <= (bound + 3 * sums) * want).all()
+    assert not da[0, 1:].any()
