@@ -227,8 +227,9 @@ __global__ __launch_bounds__(kThreads) void join_kernel(JoinArgs a, int tile_row
   constexpr int kPitch = kRank + 4;
   __shared__ float v[16 * kPitch];
   __shared__ f32x4 shared[kShare > 1 ? kThreads : 1];
-  const int64_t p0 = (int64_t)blockIdx.x * 16;
+  const int64_t p0 = ((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * 16;
   const int mode = blockIdx.y;
+  if (p0 >= a.positions) return;
   const int l = a.plan.tile_adapter[p0 / tile_rows];
   if (l < 0) return;
   const int tid = threadIdx.x;
@@ -332,7 +333,10 @@ hipError_t launch_adapter_shrink(const ShrinkArgs& a, int tile_rows, int64_t til
 }
 
 hipError_t launch_adapter_join(const JoinArgs& a, int tile_rows, hipStream_t stream) {
-  const dim3 grid((unsigned)(a.positions / 16), a.t_in ? 2 : 1);
+  // a dimension of a launch holds less than 2^32 threads
+  constexpr int64_t kMost = int64_t(1) << 23;
+  const int64_t blocks = a.positions / 16, x = blocks < kMost ? blocks : kMost;
+  const dim3 grid((unsigned)x, a.t_in ? 2 : 1, (unsigned)((blocks + x - 1) / x));
   switch (padded_rank(a.rank)) {
     case 16: join_kernel<16><<<grid, kThreads, 0, stream>>>(a, tile_rows); break;
     case 32: join_kernel<32><<<grid, kThreads, 0, stream>>>(a, tile_rows); break;
