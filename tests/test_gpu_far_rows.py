@@ -46,3 +46,37 @@ def test_adapter_on_the_most_rows():
     assert not t[:, 2:].any()
     want = torch.where(index == 0, 4 * value, torch.where(index == 1, -6 * value, zero))
     assert torch.equal(out[:, 0], want.float())
+
+
+def test_adapter_backward_on_the_most_rows():
+    """The same for the backward pass: dx of every row, and gradients whose sums
+    a few rows at both ends make up."""
+    import paper_2605_31035_amd as M
+    rows, bf = 1 << 28, torch.bfloat16
+    value = torch.arange(rows, dtype=torch.int32, device="cuda") % 5
+    index = value - 3                        # none for 0 .. 2, then 0 and 1
+    dy = value.to(bf)[:, None].expand(rows, 8).contiguous()[:, :1]
+    some = torch.tensor([3, 4, 8, rows - 30, rows - 27, rows - 3, rows - 2, rows - 1], device="cuda")
+    x = torch.zeros((rows, 8), dtype=bf, device="cuda")
+    t = torch.zeros((rows, 8), device="cuda")
+    x[some, 5], t[some, 1] = 2.0, 3.0
+    a = torch.zeros((2, 8, 8), dtype=bf, device="cuda")
+    a[0, 0, 3], a[1, 1, 7] = 1.0, 2.0
+    b = torch.zeros((2, 1, 8), dtype=bf, device="cuda")
+    b[0, 0, 0], b[1, 0, 1] = 4.0, -1.0
+    plan = M.mixfp4_adapter_plan(index, 2)
+    dx, da, db = M.mixfp4_adapter_backward(dy, x, t, a, b, plan)
+    del plan, dy, x, t
+    zero = torch.zeros_like(value)
+    for column, want in ((3, torch.where(index == 0, 4 * value, zero)),
+                         (7, torch.where(index == 1, -2 * value, zero))):
+        assert torch.equal(dx[:, column], want.float())
+        dx[:, column] = 0
+    assert not dx.any()
+    wa, wb = torch.zeros_like(da), torch.zeros_like(db)
+    for i in some.tolist():
+        v = i % 5
+        if v >= 3:
+            wa[v - 3, v - 3, 5] += 2 * v * (4 if v == 3 else -1)
+            wb[v - 3, 0, 1] += 3 * v
+    assert wa.any() and torch.equal(da, wa) and torch.equal(db, wb)
