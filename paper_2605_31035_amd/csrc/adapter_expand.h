@@ -261,6 +261,7 @@ __device__ __forceinline__ void expand_body(const ExpandArgs& a, int width, int 
           }
         }
       }
+      if (!kAhead) load_w(block + 128, more);
       // An infinite W times a second term of zero, or of the other sign than
       // the first, is NaN where the product is infinite: what is NaN is made
       // again of the first terms, whose products have the infinities and NaN of
@@ -287,7 +288,6 @@ __device__ __forceinline__ void expand_body(const ExpandArgs& a, int width, int 
             for (int e = 0; e < 4; ++e) acc[i][j][e] = acc[i][j][e] == acc[i][j][e] ? acc[i][j][e] : first[e];
           }
       }
-      if (!kAhead) load_w(block + 128, more);
 #pragma unroll
       for (int i = 0; i < kRows; ++i) {
         if constexpr (kDx) {
