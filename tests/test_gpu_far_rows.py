@@ -10,6 +10,16 @@ from tests._gpu import host
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def memory():
+    """These batches take up to 125 GB: none of it stays with torch's allocator,
+    whose large free blocks other tests would allocate in."""
+    torch.cuda.empty_cache()
+    yield
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+
+
 def test_dropout_groups_past_32_bits():
     """2^32 rows and more of one element, each a group of draws: the counter's
     high word counts."""
