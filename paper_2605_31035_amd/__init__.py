@@ -29,6 +29,9 @@ Functions (same names as the C ABI in include/mixfp4.h):
   mixfp4_adapter(x, a, b, plan, c=None, ...) -> c + scaling dropout(x) A^T B^T,
       each row with its own low-rank adapter
   mixfp4_adapter_backward(dy, x, t, a, b, plan, dx=None, ...) -> (dx, da, db)
+
+No function records itself for autograd: results do not require a gradient,
+whatever the inputs say, and a training loop calls the backward passes itself.
 """
 from __future__ import annotations
 

@@ -12,9 +12,9 @@ namespace mixfp4 {
 // A wave takes 32 columns of a block of 128, and all rows of the tile, or half
 // of them: of a tile of 64 rows, whose sums and base would hold half of the
 // registers, so that too few waves are there to hide the memory's latency
-// (1537x4096 rank 256: 67 -> 55 us, 2048x11008 rank 64: 61 -> 59).  The input
-// gradient with a small rank gains nothing by it (its draws need more
-// registers): 8192x4096 rank 64 57 us either way.
+// (whole forward passes: 1537x4096x4096 rank 256 67 -> 55 us, 2048x4096x11008
+// rank 64 61 -> 59).  The input gradient with a small rank gains nothing by it
+// (its draws need more registers): 8192x4096 rank 64 57 us either way.
 constexpr int threads_of(int tile_rows, int rank, bool dx) {
   return tile_rows == 64 && (!dx || rank > 64) ? 512 : 256;
 }
@@ -43,7 +43,7 @@ constexpr int expand_lds(int tile_rows, int rank, bool dx) {
 // in place of one that is not (behind the last block, from one address): with
 // loads in a branch each wait would have to assume that none are under way.
 // Only tiles and blocks that are not full look at each store.  Bound by
-// memory: 8192x14336 rank 64 164 us, 5.7 TB/s; 2048x11008 40 us, 4.5 TB/s.
+// memory: 8192x14336 rank 64 162 us, 5.8 TB/s; 2048x11008 40 us, 4.5 TB/s.
 template <int kT, int kRank, bool kDx, bool kOut16, bool kAligned, bool kJoin>
 __device__ __forceinline__ void expand_body(const ExpandArgs& a, int width, int tile, int chunk,
                                             uint4* lds) {
@@ -265,7 +265,8 @@ __device__ __forceinline__ void expand_body(const ExpandArgs& a, int width, int 
       // An infinite W times a second term of zero, or of the other sign than
       // the first, is NaN where the product is infinite: what is NaN is made
       // again of the first terms, whose products have the infinities and NaN of
-      // the whole.
+      // the whole.  To look costs nothing where memory bounds, and up to 1 of
+      // 41 us where few waves with a rank above 128 wait for their products.
       bool lost = false;
 #pragma unroll
       for (int e = 0; e < 8 * kRows; ++e) {

@@ -58,12 +58,13 @@ int adapter_expand_width(const ExpandArgs& a, int tile_rows, int64_t tiles, bool
   // Blocks of 128 columns per workgroup: several, so that the terms are read
   // seldom and a block's memory is requested under the one before, as long as
   // the device stays full.  A rank above 128 leaves room for one workgroup per
-  // compute unit: as many as there are units (1537x4096 rank 256: 55 us with
-  // one block each, 46 with four, 49 with five).  Else two (8192x14336 rank 64:
-  // 200 us with one, 191 with two, 204 with three), one below 6000 workgroups
-  // (2048x11008: the same with one to three); the input gradient pays more for
-  // a workgroup's start (8192x4096: 62 us with one, 56 with two).  Tiles of 16
-  // rows: 1024 workgroups (48x11008 rank 64: 22 us with one, 19 with three).
+  // compute unit: as many as there are units (the forward pass of
+  // 1537x4096x4096 rank 256: 55 us with one block each, 46 with four, 49 with
+  // five).  Else two (that of 8192x4096x14336 rank 64: 200 us with one, 191 with
+  // two, 204 with three), one below 6000 workgroups (2048x4096x11008: the same
+  // with one to three); the input gradient pays more for a workgroup's start
+  // (by itself 8192x4096: 62 us with one, 56 with two).  Tiles of 16 rows: 1024
+  // workgroups (the pass of 48x4096x11008 rank 64: 22 us with one, 19 with three).
   const bool small = tile_rows == 16;
   const int64_t blocks = (a.cols + 127) / 128, units = blocks * tiles;
   int64_t w;

@@ -29,10 +29,10 @@ __device__ __forceinline__ int64_t piece_begin(int64_t tiles, int s, int splits)
 // multiplied.  An adapter within one piece is written at once, one across
 // pieces as partial sums (at most two per piece: the one that enters it and
 // the one that leaves it) for sum_kernel.  A rank above 128 takes two
-// workgroups (r0), so that the sums stay in registers.  By themselves
-// 8192x(4096 + 14336) rank 64 take 100 us, 3.0 TB/s (56 us with rank 16): one
-// step's rows under way per workgroup and the products' LDS reads, three
-// terms of t or u for each of x or dy.
+// workgroups (r0), so that the sums stay in registers.  Bound by one step's
+// rows under way per workgroup and the products' LDS reads, three terms of t
+// or u for each of x or dy: 2048x(4096 + 4096) by themselves 34 us with rank
+// 128, 54 with 256.
 template <int kRank, bool kDb>
 __device__ __forceinline__ void grad_body(const GradSide& a, const GradArgs& q, int block, int piece,
                                           int r0, uint4* lds) {
